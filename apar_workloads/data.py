@@ -63,11 +63,12 @@ def round_to_fp8_grid(x: np.ndarray) -> np.ndarray:
 
 def quantise(x: np.ndarray, dtype: str, kv: bool = False) -> np.ndarray:
     """Round fp32 values to what a pool of the given type holds and return them as fp32 (exactly representable).
-    kv: the values are K or V rows (only matters for "bf16_fp8kv", whose queries and outputs are plain bf16)."""
+    kv: the values are K or V rows (only matters for "bf16_fp8kv", whose queries and outputs are plain bf16; rows for "bf16_fp4kv"
+    are bf16 ones, which the library rounds as oracle.fp4 does)."""
     x = np.ascontiguousarray(x, dtype=np.float32)
     if dtype == "f32":
         return x
-    if dtype == "bf16" or (dtype == "bf16_fp8kv" and not kv):
+    if dtype in ("bf16", "bf16_fp4kv") or (dtype == "bf16_fp8kv" and not kv):
         return bf16_bits_to_f32(round_to_bf16_bits(x))
     if dtype == "bf16_fp8kv":
         return round_to_fp8_grid(x)

@@ -22,7 +22,7 @@ class HeadConfig:
     n_q_heads: int
     n_kv_heads: int
     head_dim: int
-    dtype: str  # "f32", "bf16" or "bf16_fp8kv" (bf16 at the interface, full blocks cached in fp8)
+    dtype: str  # "f32", "bf16", "bf16_fp8kv" or "bf16_fp4kv" (bf16 at the interface, full blocks cached in fp8, rows in 4 bits)
     block_size: int = 16
 
     @property

@@ -71,15 +71,24 @@ typedef enum apar_status {
  * attention then reads half the bytes per cached token (Sec. 3.3 measures throughput against the memory the
  * KV cache takes).  The kernels multiply the stored codes by the scale on their way into the bf16 matrix-core
  * operands, so the arithmetic is that of a bf16 pool holding the rounded values.  Blocks keep their bf16
- * size in the pool buffer (a block must be able to hold sixteen bf16 rows while it fills). */
-enum { APAR_F32 = 0, APAR_BF16 = 1, APAR_BF16_FP8KV = 2 };
+ * size in the pool buffer (a block must be able to hold sixteen bf16 rows while it fills).
+ *
+ * APAR_BF16_FP4KV: bf16 at the interface too; every row is kept in 4 bits from the call that appends it on.  The values of
+ * a row of a kv head, K and V each, are rounded in four groups of 32 consecutive ones: to OCP e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and
+ * their negatives; round to nearest even) times 2^e, the smallest power of two with max|x| / 2^e <= 6, -120 <= e <= 125
+ * (e = 0 for a group of zeros).  The format has no infinities and no NaN: values beyond 6 * 2^125, infinities included, are held as that,
+ * NaN as 0.  A block takes APAR_FP4_TILE_BYTES per kv head in the pool buffer instead of the 8192 of a bf16 pool, and decode attention
+ * reads 136 bytes per cached token and kv head instead of 512.  The kernels' arithmetic is that of a bf16 pool holding the rounded
+ * values, but for the products of queries and keys, whose sums the matrix cores keep to about 20 bits of the largest term. */
+enum { APAR_F32 = 0, APAR_BF16 = 1, APAR_BF16_FP8KV = 2, APAR_BF16_FP4KV = 3 };
+#define APAR_FP4_TILE_BYTES 2176
 
 typedef struct apar_pool_config {
     int32_t n_q_heads;   /* Hq; multiple of n_kv_heads                                   */
     int32_t n_kv_heads;  /* Hkv                                                          */
-    int32_t head_dim;    /* d: 128 for APAR_BF16 and APAR_BF16_FP8KV; 64 or 128 for APAR_F32 */
+    int32_t head_dim;    /* d: 64 or 128 for APAR_F32; 128 for the others                 */
     int32_t block_size;  /* tokens per KV block; must be 16                              */
-    int32_t dtype;       /* APAR_F32, APAR_BF16 or APAR_BF16_FP8KV (bf16 at the interface) */
+    int32_t dtype;       /* APAR_F32, APAR_BF16, APAR_BF16_FP8KV or APAR_BF16_FP4KV        */
     int32_t max_threads; /* upper bound on ids ever issued by this pool                  */
     int64_t num_blocks;  /* N: blocks in the pool, at most 2^26                          */
     float softmax_scale; /* 0 means 1/sqrt(head_dim)                                     */
@@ -92,7 +101,7 @@ typedef struct apar_stats {
     int64_t live_threads;
     int64_t threads_issued;
     int64_t cow_copies;     /* copy-on-write block copies since creation                 */
-    int64_t block_bytes;    /* 2 * Hkv * 16 * d * element size                           */
+    int64_t block_bytes;    /* 2 * Hkv * 16 * d * element size (4-bit pools: Hkv * APAR_FP4_TILE_BYTES) */
     int64_t bytes_resident; /* used_blocks * block_bytes                                 */
     int64_t bytes_vanilla;  /* sum over live threads of ceil(len/16) * block_bytes: what */
                             /* a layout that copies the prefix on every fork would hold  */
@@ -111,7 +120,8 @@ typedef struct apar_plan_info {
     int64_t algorithmic_bytes; /* unique_tokens * 2*Hkv*d*e + q read + output written    */
                                /* (+ candidates' k, v for the multi-candidate call); on  */
                                /* an fp8 pool the tokens of full blocks count 1 byte per */
-                               /* element plus 8 bytes of scales per (block, kv head)    */
+                               /* element plus 8 bytes of scales per (block, kv head), on a */
+                               /* 4-bit pool a token 136 bytes per kv head               */
 } apar_plan_info;
 
 /* Device time measured with HIP events on the caller's stream while profiling is on. */

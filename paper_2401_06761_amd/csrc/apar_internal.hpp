@@ -40,7 +40,19 @@ static_assert(kMaxPoolBlocks * kBlockTokens <= kCodeSealed, "a slot code must no
 // of a lane is the 8 bytes at  half + (r/2)*1024 + lane*16 + (r%2)*8  (a 16-byte load brings two
 // pieces).  Bytes [4096, 4104) hold two floats, the scale of the K half and of the V half: powers
 // of two, value = code * scale.  The rest of the 8 KiB tile is unused while the block is sealed.
+//
+// 4-bit pools (APAR_BF16_FP4KV; d = 128; tile = 2176 bytes): every row is held as e2m1 codes, two to a byte, the even dim in the low
+// half, with a power-of-two scale per 32 consecutive dims, a byte e + 127 each.  A row is complete by itself: blocks are
+// never sealed.
+//   [0, 1024)     K codes: token t at 64 t
+//   [1024, 2048)  V codes: dims 8 c .. 8 c + 7 of token t, a word, at ((t / 4) 16 + c) 16 + (t % 4) 4
+//   [2048, 2112)  K scales: group g of token t at 4 t + g
+//   [2112, 2176)  V scales: group g of token t at (t / 4) 16 + 4 g + t % 4; 0 for slots that are not written yet
+// so that one 16-byte load per lane and half brings a tile as the matrix instructions take it (lane = 16 g + c: group g of K row
+// c; eight dims of four V rows) and an appended row is 64 bytes of K and sixteen words of 256 bytes of V per head.  With V
+// codes row by row a lane's share would be four loads of four bytes.
 // ---------------------------------------------------------------------------
+constexpr int kFp4V = 1024, kFp4KScale = 2048, kFp4VScale = 2112, kFp4TileBytes = 2176;
 constexpr int kFp8HalfBytes = 2048;   // one half (K or V) of a sealed fp8 tile
 constexpr int kFp8ScaleOfs = 4096;    // float K scale, float V scale
 __host__ __device__ inline int fp8_k_offset(int token, int dim) {  // byte offset of an element inside the K half
@@ -224,8 +236,9 @@ struct Shape {
     int32_t n_q, n_kv, d, group;  // group = n_q / n_kv
     int32_t dtype;                // element type of rows at the interface and in blocks that are still filling: APAR_F32 or APAR_BF16
     int32_t fp8_sealed;           // 1: full blocks are kept in fp8 with a power-of-two scale per (block, kv head) and half
+    int32_t fp4;                  // 1: all rows are kept in 4 bits with a power-of-two scale per 32 values
     float scale_log2e;            // softmax scale * log2(e): logits are kept in base 2
-    int64_t tile_bytes;           // one (block, kv head): 2 * 16 * d * e
+    int64_t tile_bytes;           // one (block, kv head): 2 * 16 * d * e, 2176 on 4-bit pools
     int64_t block_bytes;          // n_kv tiles
 };
 
@@ -284,7 +297,7 @@ constexpr size_t kSplitCounterBytes = (size_t)kSplitMaxCut * 4 * sizeof(int32_t)
 hipError_t fixed_workspace_of_device(int device, char** out);
 
 // ---- launchers (defined next to their kernels) ------------------------------
-// words: n_blocks AppendBlocks, the n_open that stay open first, then n_src source rows; on the host (at most kAppendInlineWords words, or,
+// words: n_blocks AppendBlocks, the n_open that stay open (4-bit pools: that are not written whole) first, then n_src source rows; on the host (at most kAppendInlineWords words, or,
 // without source rows on 16-bit pools, blocks that append_run takes, which go along with the kernel's arguments) or on the device.
 hipError_t launch_append_blocks(const Shape& s, void* pool, const void* k, const void* v, const int32_t* words, bool on_host,
                                 int n_blocks, int n_open, int n_src, hipStream_t st);
@@ -314,6 +327,13 @@ hipError_t launch_attention_few_bf16(const Shape& s, const void* pool, const voi
                                      const void* cand_k, const void* cand_v, const uint8_t* mask, void* out, hipStream_t st);
 hipError_t launch_attention_f32(const Shape& s, const void* pool, const void* q, const PlanDev& plan, int n_cand,
                                 PartialBuf part, const void* cand_k, const void* cand_v, const uint8_t* mask, void* out,
+                                hipStream_t st);
+hipError_t launch_attention_fp4(const Shape& s, const void* pool, const void* q, const PlanDev& plan, int n_cand,
+                                PartialBuf part, const void* cand_k, const void* cand_v, const uint8_t* mask, void* out,
+                                hipStream_t st);
+hipError_t launch_append_fp4(const Shape& s, void* pool, const void* k, const void* v, const int32_t* words, bool on_host,
+                             int n_blocks, int n_open, int n_src, hipStream_t st);
+hipError_t launch_read_rows_fp4(const Shape& s, const void* pool, const int32_t* src_codes, int n_rows, void* k_out, void* v_out,
                                 hipStream_t st);
 hipError_t launch_prefill_bf16(const Shape& s, const void* pool, const void* q, const PrefillWg* wgs,
                                const int32_t* tables, int n_wg, void* out, hipStream_t st);

@@ -85,7 +85,9 @@ struct apar_pool {
     // stand-alone segments with at least this many query rows and blocks run as matrix units (bf16 pools)
     int matrix_min_rows = 256, matrix_min_blocks = 128;
     bool inline_shared = true;  // subtrees with too many rows are cut by rank into direct units instead of leaving partial results
-    bool has_matrix_units() const { return shape.dtype == APAR_BF16 && !shape.fp8_sealed; }  // (the 32x32 kernels read bf16 tiles only)
+    bool has_matrix_units() const { return shape.dtype == APAR_BF16 && !shape.fp8_sealed && !shape.fp4; }  // (the 32x32 kernels read bf16 tiles only)
+    // kernels that read tiles as they are, wavefront by wavefront: all tiles are alike, shared lists are staged for nobody
+    bool reads_tiles_alone() const { return shape.dtype == APAR_F32 || shape.fp4; }
     bool check_writes = false;  // verify before every launch that no destination block is shared
     int last_prefill_kernel = 0;  // which kernel the most recent prefill call ran (APAR_PREFILL_ROW_TILES / _MATRIX)
     std::vector<PlanThreadView> views;
@@ -381,7 +383,10 @@ int run_append(apar_pool* p, const std::vector<int32_t>& codes, const std::vecto
     const size_t copy_words = copies_first ? copies.size() : 0;
     bool inlined = words <= (size_t)kAppendInlineWords && copy_words == 0;
     if (p->shape.dtype != APAR_F32) {
-        auto stays_open = [](const AppendBlock& b) { return b.slots >> 8 < kBlockTokens; };
+        const bool fp4 = p->shape.fp4 != 0;  // (nothing is sealed: whole blocks have a kernel of their own)
+        auto stays_open = [fp4](const AppendBlock& b) {
+            return fp4 ? b.slots != kBlockTokens << 8 || b.copy_of >= 0 : b.slots >> 8 < kBlockTokens;
+        };
         const bool maybe_run = !inlined && copy_words == 0 && src.empty();
         n_open = (int)((maybe_run ? std::stable_partition(blocks.begin(), blocks.end(), stays_open)
                                   : std::partition(blocks.begin(), blocks.end(), stays_open)) -
@@ -643,12 +648,12 @@ int decode_common(apar_pool* p, const void* q, const void* cand_k, const void* c
     prm.matrix_min_rows = p->has_matrix_units() ? p->matrix_min_rows : 0;
     prm.matrix_min_blocks = p->matrix_min_blocks;
     prm.inline_shared = p->inline_shared;
-    prm.open_cost = p->shape.dtype == APAR_F32 ? 1 : kOpenTileCost;
+    prm.open_cost = p->reads_tiles_alone() ? 1 : kOpenTileCost;
     prm.few_units = p->planning_set ? 0 : kFewUnits / p->shape.n_kv;
-    // (the fp32 kernel's wavefronts read shared lists one by one: units of 16 rows read nothing more often)
-    const int64_t tile_read = p->shape.n_kv * (p->shape.fp8_sealed ? 4096 : 8192);
-    prm.few_row_tiles = p->shape.dtype == APAR_F32 ? 1 : 2;
-    prm.few_again = p->shape.dtype == APAR_F32 ? INT32_MAX : (int32_t)(kFewAgainBytes / tile_read);
+    // (wavefronts of the fp32 and 4-bit kernels read shared lists one by one: units of 16 rows read nothing more often)
+    const int64_t tile_read = p->shape.n_kv * (p->shape.fp4 ? kFp4TileBytes : p->shape.fp8_sealed ? 4096 : 8192);
+    prm.few_row_tiles = p->reads_tiles_alone() ? 1 : 2;
+    prm.few_again = p->reads_tiles_alone() ? INT32_MAX : (int32_t)(kFewAgainBytes / tile_read);
     prm.few_again_wide = (int32_t)(kFewAgainWideBytes / tile_read);
     prm.few_again_narrow = (int32_t)(kFewAgainNarrowBytes / tile_read);
     prm.few_small = (int32_t)(kFewSmallBytes / tile_read);
@@ -689,6 +694,8 @@ int decode_common(apar_pool* p, const void* q, const void* cand_k, const void* c
     info.path_tokens = ph.path_tokens;
     info.algorithmic_bytes = ph.unique_tokens * 2 * p->shape.n_kv * p->shape.d * e +
                              2 * (int64_t)n * n_cand * p->shape.n_q * p->shape.d * e;
+    if (p->shape.fp4)  // four bits per element and a byte per 32
+        info.algorithmic_bytes -= ph.unique_tokens * p->shape.n_kv * (2 * p->shape.d * e - kFp4TileBytes / kBlockTokens);
     if (p->shape.fp8_sealed)  // full blocks: one byte per element and two scales per (block, kv head)
         info.algorithmic_bytes -= ph.full_blocks * ((int64_t)kBlockTokens * p->shape.n_kv * p->shape.d * 2 - 8 * p->shape.n_kv);
     if (spec) info.algorithmic_bytes += 2 * (int64_t)n * n_cand * p->shape.n_kv * p->shape.d * e;
@@ -702,7 +709,7 @@ int decode_common(apar_pool* p, const void* q, const void* cand_k, const void* c
     DeviceGuard guard(p->device);
     hipStream_t st = (hipStream_t)stream;
 
-    const bool few = ph.few_row_tiles > 0 && p->shape.dtype != APAR_F32;  // (fp32 pools have one kernel for all units)
+    const bool few = ph.few_row_tiles > 0 && !p->reads_tiles_alone();  // (those pools have one kernel for all units)
     if (!carried) cut_into_slices(ph, p->shape, few, p->split_bytes, p->split_blocks, p->n_split_class);  // (a carried plan keeps its cut)
     // stage the tables in one copy
     size_t ofs[7];
@@ -902,7 +909,7 @@ bool prefill_on_matrix(const Shape& s, const std::vector<PrefillThreadView>& vie
         ((int64_t)t.m * s.group > kMatrixPrefillRows ? wide : narrow) += w * (t.len - t.m) + chunk * (w - 1) * w / 2 + t.m;
     }
     if (wide >= narrow) return true;
-    if (s.fp8_sealed) return false;
+    if (s.fp8_sealed || s.fp4) return false;
     return attended >= kMatrixPrefillMeanWalk * rows ||
            (rows * s.group >= kMatrixPrefillMinRows * wgs && (wide + narrow) * s.n_kv >= kMatrixPrefillWalked);
 }
@@ -1016,7 +1023,7 @@ int prefill_common(apar_pool* p, const void* q, const apar_thread* ids, const in
     int rc = APAR_OK;
     p->last_prefill_kernel = APAR_PREFILL_ROW_TILES;
     // (an fp8 pool takes the matrix kernel by AUTO only)
-    if (!p->dry_run && p->shape.dtype == APAR_BF16 && 16 % p->shape.group == 0 &&
+    if (!p->dry_run && p->shape.dtype == APAR_BF16 && !p->shape.fp4 && 16 % p->shape.group == 0 &&
         ((p->prefill_kernel == APAR_PREFILL_MATRIX && !p->shape.fp8_sealed) ||
          (p->prefill_kernel == APAR_PREFILL_AUTO && prefill_on_matrix(p->shape, views, rows, attended)))) {
         p->last_prefill_kernel = APAR_PREFILL_MATRIX;
@@ -1090,13 +1097,14 @@ int apar_pool_create(const apar_pool_config* cfg, void* kv_dev, size_t kv_bytes,
     if (cfg->n_q_heads < 1 || cfg->n_kv_heads < 1 || cfg->n_q_heads % cfg->n_kv_heads) return APAR_ERR_INVALID_ARG;
     if (cfg->num_blocks < 1 || cfg->num_blocks > kMaxPoolBlocks || cfg->max_threads < 1)
         return APAR_ERR_INVALID_ARG;
-    if (cfg->dtype != APAR_F32 && cfg->dtype != APAR_BF16 && cfg->dtype != APAR_BF16_FP8KV) return APAR_ERR_INVALID_ARG;
+    if (cfg->dtype != APAR_F32 && cfg->dtype != APAR_BF16 && cfg->dtype != APAR_BF16_FP8KV && cfg->dtype != APAR_BF16_FP4KV)
+        return APAR_ERR_INVALID_ARG;
     if (!(cfg->softmax_scale >= 0.0f) || !std::isfinite(cfg->softmax_scale)) return APAR_ERR_INVALID_ARG;
     if (cfg->dtype != APAR_F32 && cfg->head_dim != 128) return APAR_ERR_UNSUPPORTED;
     if (cfg->dtype == APAR_F32 && cfg->head_dim != 64 && cfg->head_dim != 128) return APAR_ERR_UNSUPPORTED;
     if (cfg->n_q_heads / cfg->n_kv_heads > 16) return APAR_ERR_UNSUPPORTED;
     const int64_t e = cfg->dtype == APAR_F32 ? 4 : 2;
-    const int64_t tile = 2 * (int64_t)kBlockTokens * cfg->head_dim * e;
+    const int64_t tile = cfg->dtype == APAR_BF16_FP4KV ? kFp4TileBytes : 2 * (int64_t)kBlockTokens * cfg->head_dim * e;
     const int64_t block = tile * cfg->n_kv_heads;
     if (kv_dev && ((uint64_t)kv_bytes < (uint64_t)(block * cfg->num_blocks) || ((uintptr_t)kv_dev & 255)))
         return APAR_ERR_INVALID_ARG;
@@ -1129,6 +1137,7 @@ int apar_pool_create(const apar_pool_config* cfg, void* kv_dev, size_t kv_bytes,
     p->shape.group = cfg->n_q_heads / cfg->n_kv_heads;
     p->shape.dtype = cfg->dtype == APAR_F32 ? APAR_F32 : APAR_BF16;
     p->shape.fp8_sealed = cfg->dtype == APAR_BF16_FP8KV ? 1 : 0;
+    p->shape.fp4 = cfg->dtype == APAR_BF16_FP4KV ? 1 : 0;
     p->shape.scale_log2e = scale * 1.4426950408889634f;
     p->shape.tile_bytes = tile;
     p->shape.block_bytes = block;

@@ -413,6 +413,7 @@ hipError_t fixed_workspace_of_device(int device, char** out) {
 hipError_t launch_append_blocks(const Shape& s, void* pool, const void* k, const void* v, const int32_t* words, bool on_host,
                                 int n_blocks, int n_open, int n_src, hipStream_t st) {
     if (n_blocks <= 0) return hipSuccess;
+    if (s.fp4) return launch_append_fp4(s, pool, k, v, words, on_host, n_blocks, n_open, n_src, st);
     if (s.dtype == APAR_F32 && n_open != n_blocks) return hipErrorInvalidValue;  // (fp32 blocks are never sealed)
     const int pairs = s.dtype == APAR_F32 && s.d == 128 ? 4 : 8;
     const int64_t grid = ((int64_t)n_open * s.n_kv + pairs - 1) / pairs + ((int64_t)(n_blocks - n_open) * s.n_kv + 3) / 4;
@@ -515,6 +516,7 @@ hipError_t launch_clear_words(int32_t* words, int n, hipStream_t st) {
 hipError_t launch_read_rows(const Shape& s, const void* pool, const int32_t* src_codes, int n_rows, void* k_out,
                             void* v_out, hipStream_t st) {
     if (n_rows <= 0) return hipSuccess;
+    if (s.fp4) return launch_read_rows_fp4(s, pool, src_codes, n_rows, k_out, v_out, st);
     dim3 grid(n_rows, s.n_kv);
     if (s.dtype == APAR_BF16)
         hipLaunchKernelGGL(read_rows_bf16, grid, dim3(64), 0, st, (const char*)pool, (uint16_t*)k_out,
@@ -529,6 +531,7 @@ hipError_t launch_attention_partial(const Shape& s, const void* pool, const void
                                     PartialBuf part, const void* cand_k, const void* cand_v, const uint8_t* mask,
                                     void* out, hipStream_t st) {
     if (plan.n_wg <= 0) return hipSuccess;
+    if (s.fp4) return launch_attention_fp4(s, pool, q, plan, n_cand, part, cand_k, cand_v, mask, out, st);
     if (s.dtype == APAR_BF16)
         return launch_attention_bf16(s, pool, q, plan, n_cand, part, cand_k, cand_v, mask, out, st);
     return launch_attention_f32(s, pool, q, plan, n_cand, part, cand_k, cand_v, mask, out, st);
