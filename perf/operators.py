@@ -256,7 +256,7 @@ def prepare(case, seed):
                                     low_turns=1.0, high_turns=32.0, magnitude=s["magnitude"])
             if kind == "step":  # one thread that grows, a child forked off it at every row's position
                 at = s["positions"].tolist()
-                s["pool"] = pool = ap.Pool(hq, hkv, D, "bf16_fp4kv", at[-1] // 16 + 2, max_threads=n + 1, device=DEV)
+                s["pool"] = pool = ap.Pool(hq, hkv, D, "bf16_fp4kv", at[-1] // 16 + 2 + n, max_threads=n + 1, device=DEV)
                 root, s["threads"] = ap.apar_thread_create(pool.handle), []
                 rows = torch.zeros(max(1, at[-1]), hkv, D, dtype=dtype, device=DEV)
                 have = 0
