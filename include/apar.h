@@ -288,6 +288,63 @@ APAR_API int apar_commit_candidates(apar_pool* pool, const apar_thread* threads,
 APAR_API int apar_prefill_attention(apar_pool* pool, const void* q_dev, const apar_thread* threads, const int32_t* m,
                            int n, void* out_dev, void* hip_stream);
 
+/*
+ * Rotary positions.  Keys are cached as they are given, and attention knows no positions (a thread's rows are a set), so a model with
+ * rotary positions turns its query and key rows before apar_append_kv and the attention calls: pair i (i < rotary_dim / 2) of every head
+ * by the angle position * theta_i,
+ *   y_a = s (x_a cos - x_b sin),  y_b = s (x_b cos + x_a sin),   s = magnitude,
+ * computed in 64 bits as far as the fraction of a turn, then in 32, and rounded once.  The dims behind rotary_dim stay as they are.
+ *   layout   APAR_ROTARY_HALF: (a, b) = (i, i + rotary_dim / 2);  APAR_ROTARY_PAIRS: (2 i, 2 i + 1)
+ *   scaling  of theta_i = base^(-2 i / rotary_dim) for long contexts:
+ *     NONE;  LINEAR theta_i / factor;  BASE: base * factor^(rotary_dim / (rotary_dim - 2)) in place of base;
+ *     RAMP: k theta_i + (1 - k) theta_i / factor with k = clamp((n - low_turns) / (high_turns - low_turns), 0, 1), n = original_len
+ *     theta_i / (2 pi), the turns that the pair makes over the original length.
+ *   transposed != 0 turns the other way (sin -> -sin, s stays): the gradient of x for a gradient of y, and, with s = 1, the way back.
+ */
+typedef struct apar_rotary apar_rotary; /* host memory only; may be used by any number of calls */
+enum { APAR_ROTARY_HALF = 0, APAR_ROTARY_PAIRS = 1 };
+enum { APAR_ROTARY_SCALE_NONE = 0, APAR_ROTARY_SCALE_LINEAR = 1, APAR_ROTARY_SCALE_BASE = 2, APAR_ROTARY_SCALE_RAMP = 3 };
+typedef struct apar_rotary_config {
+    int32_t head_dim;    /* d; even, at most 256 (UNSUPPORTED beyond)                    */
+    int32_t rotary_dim;  /* the first dims of a head that are turned; even, 2 .. d       */
+    int32_t layout, scaling;
+    double base;         /* > 0, e.g. 10000                                              */
+    double factor;       /* > 0; LINEAR, BASE, RAMP                                      */
+    double original_len, low_turns, high_turns; /* RAMP: > 0; low_turns < high_turns     */
+    double magnitude;    /* > 0; 1 for none                                              */
+} apar_rotary_config;
+/* Rows of a call: row i starts i * in_stride (out_stride) elements behind in_dev (out_dev), heads side by side, head_dim elements each.
+ * out_dev may be in_dev, with equal strides; the two may not overlap in any other way. */
+typedef struct apar_rotary_rows {
+    const void* in_dev;
+    void* out_dev;
+    int64_t in_stride, out_stride; /* at least n_heads * head_dim */
+    int32_t n_heads;
+} apar_rotary_rows;
+APAR_API int apar_rotary_create(const apar_rotary_config* cfg, apar_rotary** out);
+APAR_API int apar_rotary_destroy(apar_rotary* rotary); /* NULL is accepted */
+/* theta_i as the calls use it; n_out is always set (INVALID_ARG if cap is too small). */
+APAR_API int apar_rotary_frequencies(const apar_rotary* rotary, double* out, int cap, int* n_out);
+/* Rows at positions_dev[0 .. n_rows) (device; any int32).  dtype: APAR_F32 or APAR_BF16, of both; q or k may be NULL.  One launch, nothing
+ * allocated: may be captured into a graph.  Errors: INVALID_ARG, UNSUPPORTED, HIP. */
+APAR_API int apar_rotate_rows(const apar_rotary* rotary, int dtype, const int32_t* positions_dev, int64_t n_rows,
+                              const apar_rotary_rows* q, const apar_rotary_rows* k, int transposed, void* hip_stream);
+/*
+ * Rows of listed threads, whose positions are in the pool's books: m[i] rows (1 each if m is NULL) of thread i, thread by thread.
+ *   APAR_ROWS_NEXT  rows that are about to be appended, in this order: they follow the thread's len rows, and the rows of earlier
+ *                   entries of the same thread.  m[i] >= 0.
+ *   APAR_ROWS_LAST  the thread's last m[i] rows (1 .. len), as for apar_prefill_attention.
+ *   n_cand > 0      candidates ([n, n_cand] rows, mask_dev as for apar_decode_attention_spec, NEXT, m NULL): a candidate lies as
+ *                   many positions behind the thread's rows as it sees other candidates.
+ * dtype (of the rows: APAR_F32 on fp32 pools, APAR_BF16 on the others), numbers of heads and head_dim are the pool's.  Enqueues one launch, and an upload of a word or two per thread where there
+ * are more than some 250 of them.  On a dry-run pool q, k and mask_dev are NULL.
+ * Errors: INVALID_THREAD, INVALID_ARG, UNSUPPORTED (positions or rows past 2^31), HIP.
+ */
+enum { APAR_ROWS_NEXT = 0, APAR_ROWS_LAST = 1 };
+APAR_API int apar_rotate_threads(apar_pool* pool, const apar_rotary* rotary, int dtype, const apar_thread* threads, const int32_t* m, int n, int where,
+                                 const uint8_t* mask_dev, int n_cand, const apar_rotary_rows* q, const apar_rotary_rows* k, int transposed,
+                                 void* hip_stream);
+
 /* Release (Alg. 1 ReleaseCache): walks the table from its last block to its
  * first, drops one reference from each and returns a block to the pool when no
  * thread holds it any more.  Errors: INVALID_THREAD. */

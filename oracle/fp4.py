@@ -37,5 +37,7 @@ def held(x: np.ndarray) -> np.ndarray:
     x[np.isnan(x)] = 0.0
     x = np.clip(x, -MOST, MOST)
     g = x.reshape(-1, 32)
-    e = np.array([group_exponent(t) for t in np.abs(g).max(axis=1)], dtype=np.float64)[:, None]
+    top = np.abs(g).max(axis=1)
+    e = np.arange(-120, 126)[np.searchsorted(6.0 * 2.0 ** np.arange(-120.0, 126.0), top, side="left")]
+    e = np.where(top > 0.0, e, 0).astype(np.float64)[:, None]
     return (nearest(g / 2.0 ** e) * 2.0 ** e).reshape(x.shape)

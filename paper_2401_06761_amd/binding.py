@@ -71,6 +71,21 @@ class AparServerStats(C.Structure):
                                          "batch_sequences_total", "peak_used_blocks", "peak_running", "peak_threads")]
 
 
+class AparRotaryConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("head_dim", "rotary_dim", "layout", "scaling")] + \
+               [(n, C.c_double) for n in ("base", "factor", "original_len", "low_turns", "high_turns", "magnitude")]
+
+
+class AparRotaryRows(C.Structure):
+    _fields_ = [("in_dev", C.c_void_p), ("out_dev", C.c_void_p), ("in_stride", C.c_int64), ("out_stride", C.c_int64),
+                ("n_heads", C.c_int32)]
+
+
+APAR_ROTARY_HALF, APAR_ROTARY_PAIRS = 0, 1
+APAR_ROTARY_SCALE_NONE, APAR_ROTARY_SCALE_LINEAR, APAR_ROTARY_SCALE_BASE, APAR_ROTARY_SCALE_RAMP = range(4)
+APAR_ROWS_NEXT, APAR_ROWS_LAST = 0, 1
+
+
 class AparProfile(C.Structure):
     _fields_ = [("n_decode_calls", C.c_int64), ("attention_kernel_ms", C.c_double), ("merge_kernel_ms", C.c_double),
                 ("plan_host_ms", C.c_double), ("n_append_calls", C.c_int64), ("append_kernels_ms", C.c_double),
@@ -105,6 +120,11 @@ def _load() -> C.CDLL:
         "apar_decode_attention_spec": [P, V, V, V, V, I, I32P, I, V, V],
         "apar_commit_candidates": [P, I32P, I, V, V, I, C.POINTER(C.c_uint8), V],
         "apar_prefill_attention": [P, V, I32P, I32P, I, V, V],
+        "apar_rotary_create": [C.POINTER(AparRotaryConfig), C.POINTER(P)],
+        "apar_rotary_destroy": [P],
+        "apar_rotary_frequencies": [P, C.POINTER(C.c_double), I, C.POINTER(C.c_int)],
+        "apar_rotate_rows": [P, I, V, C.c_int64, C.POINTER(AparRotaryRows), C.POINTER(AparRotaryRows), I, V],
+        "apar_rotate_threads": [P, P, I, I32P, I32P, I, I, V, I, C.POINTER(AparRotaryRows), C.POINTER(AparRotaryRows), I, V],
         "apar_free_thread": [P, C.c_int32],
         "apar_thread_len": [P, C.c_int32, C.POINTER(C.c_int64)],
         "apar_thread_block_table": [P, C.c_int32, I32P, I, C.POINTER(C.c_int)],
@@ -325,6 +345,113 @@ def apar_prefill_attention(pool, q, threads: Sequence[int], m: Sequence[int], ou
         raise ValueError("one m per listed thread")
     _check(_L().apar_prefill_attention(pool, _ptr(q), arr, marr, n, _ptr(out), _stream(stream)),
            "apar_prefill_attention")
+
+
+def apar_rotary_create(cfg: AparRotaryConfig) -> C.c_void_p:
+    out = C.c_void_p()
+    _check(_L().apar_rotary_create(C.byref(cfg), C.byref(out)), "apar_rotary_create")
+    return out
+
+
+def apar_rotary_destroy(rotary) -> None:
+    _check(_L().apar_rotary_destroy(rotary), "apar_rotary_destroy")
+
+
+def apar_rotary_frequencies(rotary) -> List[float]:
+    n = C.c_int()
+    _L().apar_rotary_frequencies(rotary, None, 0, C.byref(n))
+    buf = (C.c_double * max(n.value, 1))()
+    _check(_L().apar_rotary_frequencies(rotary, buf, n.value, C.byref(n)), "apar_rotary_frequencies")
+    return list(buf[: n.value])
+
+
+def _rotary_rows(x, out, n_rows: Optional[int]):
+    """A [..., heads, head_dim] tensor whose heads lie side by side; rows may be any distance apart (a slice of a wider projection)."""
+    if x is None:
+        if out is not None:
+            raise ValueError("an output without its input")
+        return None, n_rows
+    out = x if out is None else out
+
+    def layout(t):
+        if not t.is_cuda or t.dim() < 3:
+            raise ValueError("expected GPU tensors [rows, heads, head_dim]")
+        shape, stride = t.shape, t.stride()
+        if (shape[-1] > 1 and stride[-1] != 1) or (shape[-2] > 1 and stride[-2] != shape[-1]):
+            raise ValueError("the heads of a row must lie side by side")
+        for i in range(t.dim() - 3):  # leading dims that are one after the other
+            if shape[i] > 1 and stride[i] != shape[i + 1] * stride[i + 1]:
+                raise ValueError("rows must be evenly spaced")
+        n = 1
+        for s in shape[:-2]:
+            n *= s
+        row = shape[-2] * shape[-1]
+        return n, max(stride[-3], row) if n > 1 else row
+
+    n, step = layout(x)
+    if out.shape != x.shape or out.dtype != x.dtype or out.device != x.device:
+        raise ValueError("the output must have its input's shape, type and device")
+    if n_rows is not None and n != n_rows:
+        raise ValueError(f"{n} rows where {n_rows} are meant")
+    if n > 1 and (x.stride(-3) < x.shape[-2] * x.shape[-1] or out.stride(-3) < x.shape[-2] * x.shape[-1]):
+        raise ValueError("rows must not overlap")
+    return AparRotaryRows(x.data_ptr(), out.data_ptr(), step, layout(out)[1], x.shape[-2]), n
+
+
+def _stream_on(t, stream) -> int:
+    """The given stream, or the current one of the tensor's device."""
+    if stream is not None or t is None:
+        return _stream(stream)
+    import torch
+
+    return torch._C._cuda_getCurrentRawStream(t.device.index) if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
+        torch.cuda.current_stream(t.device).cuda_stream
+
+
+def _rotary_dtype(*tensors) -> int:
+    import torch
+
+    kinds = {t.dtype for t in tensors if t is not None}
+    if kinds == {torch.float32}:
+        return APAR_F32
+    if kinds == {torch.bfloat16}:
+        return APAR_BF16
+    raise ValueError("expected float32 or bfloat16, one of them")
+
+
+def apar_rotate_rows(rotary, positions, q, k=None, q_out=None, k_out=None, transposed: bool = False, stream=None) -> None:
+    """q, k: [rows, heads, head_dim] (either may be None), turned in place or into q_out, k_out; positions: [rows] int32 on the GPU."""
+    import torch
+
+    if positions.dtype != torch.int32 or positions.dim() != 1:
+        raise ValueError("positions must be a 1-d int32 tensor")
+    qr, n = _rotary_rows(q, q_out, positions.shape[0])
+    kr, n = _rotary_rows(k, k_out, positions.shape[0])
+    if any(t is not None and t.device != positions.device for t in (q, k)):
+        raise ValueError("all tensors must be on one device")
+    if qr is None and kr is None:
+        raise ValueError("neither q nor k")
+    _check(_L().apar_rotate_rows(rotary, _rotary_dtype(q, k), _ptr(positions), positions.shape[0], qr, kr, int(bool(transposed)),
+                                 _stream_on(positions, stream)), "apar_rotate_rows")
+
+
+def apar_rotate_threads(pool, rotary, threads: Sequence[int], q, k=None, q_out=None, k_out=None, m: Optional[Sequence[int]] = None,
+                        where: int = APAR_ROWS_NEXT, mask=None, n_cand: int = 0, transposed: bool = False, stream=None) -> None:
+    """Rows of listed threads at the positions that the pool's books give them (q and k None: a dry-run pool)."""
+    arr, n = _ids(threads)
+    marr, rows = None, n * max(1, n_cand)
+    if m is not None:
+        marr, nm = _ids(m)
+        if nm != n:
+            raise ValueError("one m per listed thread")
+        rows = int(sum(m))
+    dtype = _rotary_dtype(q, k) if q is not None or k is not None else APAR_BF16
+    qr, _ = _rotary_rows(q, q_out, rows)
+    kr, _ = _rotary_rows(k, k_out, rows)
+    if mask is not None and (mask.element_size() != 1 or mask.numel() != rows):
+        raise ValueError("mask must hold one byte per candidate")
+    _check(_L().apar_rotate_threads(pool, rotary, dtype, arr, marr, n, where, _ptr(mask), n_cand, qr, kr, int(bool(transposed)),
+                                    _stream_on(q if q is not None else k, stream)), "apar_rotate_threads")
 
 
 def apar_free_thread(pool, thread: int) -> None:
@@ -589,6 +716,37 @@ class Pool:
             apar_pool_destroy(self.handle)
             self.handle = None
             self.kv = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Rotary:
+    """Rotary positions of one model: owns the handle that apar_rotate_rows and apar_rotate_threads take."""
+
+    def __init__(self, head_dim: int, rotary_dim: Optional[int] = None, layout: str = "half", base: float = 10000.0, scaling: str = "none",
+                 factor: float = 1.0, original_len: float = 0.0, low_turns: float = 1.0, high_turns: float = 32.0, magnitude: float = 1.0):
+        self.handle = None
+        self.cfg = AparRotaryConfig(head_dim, head_dim if rotary_dim is None else rotary_dim,
+                                    {"half": APAR_ROTARY_HALF, "pairs": APAR_ROTARY_PAIRS}[layout],
+                                    {"none": APAR_ROTARY_SCALE_NONE, "linear": APAR_ROTARY_SCALE_LINEAR, "base": APAR_ROTARY_SCALE_BASE,
+                                     "ramp": APAR_ROTARY_SCALE_RAMP}[scaling],
+                                    base, factor, original_len, low_turns, high_turns, magnitude)
+        self.handle = apar_rotary_create(self.cfg)
+
+    def close(self) -> None:
+        if self.handle is not None:
+            apar_rotary_destroy(self.handle)
+            self.handle = None
 
     def __enter__(self):
         return self

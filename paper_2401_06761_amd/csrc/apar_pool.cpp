@@ -13,24 +13,22 @@
 #include <vector>
 
 #include "apar_internal.hpp"
+#include "hip_status.hpp"
 #include "plan.hpp"
+#include "pool_access.hpp"
 
 using namespace apar;
 
-namespace {
+static thread_local std::string g_last_hip_error;
 
-thread_local std::string g_last_hip_error;
-
-bool hip_ok(hipError_t e, const char* what) {
+bool apar::hip_ok(hipError_t e, const char* what) {
     if (e == hipSuccess) return true;
     g_last_hip_error = std::string(what) + ": " + hipGetErrorString(e);
     (void)hipGetLastError();  // (reported here: the next launch's check must not find it)
     return false;
 }
-#define HIP_TRY(expr)                                  \
-    do {                                               \
-        if (!hip_ok((expr), #expr)) return APAR_ERR_HIP; \
-    } while (0)
+
+namespace {
 
 struct Thread {
     bool live = false;
@@ -157,17 +155,6 @@ struct apar_pool {
 };
 
 namespace {
-
-struct DeviceGuard {
-    int prev = 0;
-    bool switched = false;
-    explicit DeviceGuard(int dev) {
-        if (hipGetDevice(&prev) == hipSuccess && prev != dev) switched = (hipSetDevice(dev) == hipSuccess);
-    }
-    ~DeviceGuard() {
-        if (switched) (void)hipSetDevice(prev);
-    }
-};
 
 Thread* live_thread(apar_pool* p, apar_thread t) {
     if (t < 0 || (size_t)t >= p->threads.size() || !p->threads[t].live) return nullptr;
@@ -1083,6 +1070,25 @@ int prefill_common(apar_pool* p, const void* q, const apar_thread* ids, const in
 }
 
 }  // namespace
+
+// What the operators beside the pool see of it (pool_access.hpp).
+PoolFacts apar::facts_of(const apar_pool* p) { return PoolFacts{&p->shape, p->kv, p->device, p->dry_run}; }
+
+int apar::stage_words(apar_pool* p, const int32_t* words, size_t n, hipStream_t st, StagedWords* out) {
+    StageSlot* s = nullptr;
+    const int rc = acquire_stage(p, n * sizeof(int32_t), &s);
+    if (rc != APAR_OK) return rc;
+    memcpy(s->host, words, n * sizeof(int32_t));
+    *out = StagedWords{(const int32_t*)s->dev, s};
+    return upload(p, s, n * sizeof(int32_t), st);
+}
+
+int apar::staged_words_read(const StagedWords& w, hipStream_t st) {
+    StageSlot* s = (StageSlot*)w.slot;
+    HIP_TRY(hipEventRecord(s->ev, st));
+    s->pending = true;
+    return APAR_OK;
+}
 
 // ===========================================================================
 // C ABI

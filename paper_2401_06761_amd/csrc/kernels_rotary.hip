@@ -1,0 +1,153 @@
+// Rotary positions (gfx950): q and k rows, head by head, pairs of dims turned by the angle position * theta_i.
+//
+//   y_a = s (x_a cos - x_b sin),  y_b = s (x_b cos + x_a sin)        transposed: sin -> -sin
+//
+// Angles are kept in turns and in 64 bits until the fraction of a turn is left: position * theta / 2 pi of a far position loses
+// as many bits in 32 as it has whole turns.  The fraction, at most half, is then good to 2^-26 in 32 bits, 9e-8 of angle.
+// A workgroup takes a few rows: its threads work out the sines and cosines of the rows' pairs once, in LDS, and then go through
+// all heads of those rows, 16 bytes of a's and 16 of b's a lane (the bytes of a pair's partner in another lane would need an
+// exchange).  What bounds it: memory, every row read and written once; calls of few rows: the launch.
+#include <hip/hip_runtime.h>
+
+#include <cstring>
+
+#include "apar_internal.hpp"
+#include "rotary.hpp"
+
+namespace apar {
+
+namespace {
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+template <class T>
+__device__ __forceinline__ float widened(T x);
+template <>
+__device__ __forceinline__ float widened<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ float widened<uint16_t>(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+template <class T>
+__device__ __forceinline__ T narrowed(float x);
+template <>
+__device__ __forceinline__ float narrowed<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ uint16_t narrowed<uint16_t>(float x) {  // round to nearest even
+    const f32x2 p = {x, x};
+    return (uint16_t)__builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
+}
+
+// W pairs a lane: 16 bytes of either half (1: sizes or addresses that do not allow that).  PAIRS: the dims of a pair lie side by side.
+template <class T, int W, bool PAIRS>
+__global__ __launch_bounds__(256) void rotate_rows(RotaryArgs args, RotaryCall call) {
+    extern __shared__ f32x2 turns[];  // [rows of the workgroup][pairs]: cosine, sine
+    struct __attribute__((aligned(sizeof(T) * W))) Vec {
+        T x[W];
+    };
+    const int64_t row0 = (int64_t)blockIdx.x * call.rows_per_wg;
+    const int n_rows = (int)min((int64_t)call.rows_per_wg, call.n_rows - row0);
+    const int pairs = call.rotary_dim / 2;
+    // the tables are the first argument, read where they are
+    typedef const double __attribute__((address_space(4))) * Doubles;
+    typedef const int32_t __attribute__((address_space(4))) * Words;
+    const auto theta = (Doubles)__builtin_amdgcn_kernarg_segment_ptr();
+    const auto inlined = (Words)(theta + kRotaryMaxPairs);
+    auto word = [&](int i) -> int { return call.tables ? call.tables[i] : inlined[i]; };
+    for (int at = threadIdx.x; at < n_rows * pairs; at += 256) {
+        const int r = at / pairs, i = at - r * pairs;
+        const int64_t row = row0 + r;
+        int64_t pos;
+        if (call.positions) {
+            pos = call.positions[row];
+        } else if (call.rows_per_entry > 0) {  // as many rows for every listed thread
+            const int entry = (int)(row / call.rows_per_entry);
+            pos = word(entry);
+            if (call.mask) {
+                const uint32_t seen = call.mask[row] & ((1u << call.rows_per_entry) - 1u);
+                pos += __builtin_popcount(seen) - 1;  // a candidate sees its ancestors and itself
+            } else {
+                pos += row - (int64_t)entry * call.rows_per_entry;
+            }
+        } else {  // the last listed thread whose first row is not behind this one
+            int lo = 0, hi = call.n_entries;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) / 2;
+                if (word(2 * mid) <= row) lo = mid;
+                else hi = mid;
+            }
+            pos = word(2 * lo + 1) + (row - word(2 * lo));
+        }
+        const double t = (double)pos * theta[i];
+        float s, c;
+        sincospif(2.0f * (float)(t - rint(t)), &s, &c);
+        turns[at] = f32x2{c * call.magnitude, s * (call.transposed ? -call.magnitude : call.magnitude)};
+    }
+    __syncthreads();
+    const int heads = call.q.n_heads + call.k.n_heads;
+    const int pieces = call.head_dim / (2 * W), turned = call.rotary_dim / (2 * W);  // a piece is 2 W dims of a head
+    const int total = n_rows * heads * pieces;
+    for (int at = threadIdx.x; at < total; at += 256) {
+        const int rh = at / pieces, piece = at - rh * pieces;
+        const int r = rh / heads, head = rh - r * heads;
+        const bool is_q = head < call.q.n_heads;
+        const RotaryRows& x = is_q ? call.q : call.k;
+        const int h = is_q ? head : head - call.q.n_heads;
+        const T* in = (const T*)x.in + (row0 + r) * x.in_stride + (int64_t)h * call.head_dim;
+        T* out = (T*)x.out + (row0 + r) * x.out_stride + (int64_t)h * call.head_dim;
+        if (piece >= turned) {  // dims behind the turned ones: taken over
+            if (in == out) continue;
+            const Vec u = *(const Vec*)(in + 2 * W * piece), v = *(const Vec*)(in + 2 * W * piece + W);
+            *(Vec*)(out + 2 * W * piece) = u;
+            *(Vec*)(out + 2 * W * piece + W) = v;
+            continue;
+        }
+        const int a = PAIRS ? 2 * W * piece : W * piece, b = PAIRS ? a + W : a + pairs;
+        Vec u = *(const Vec*)(in + a), v = *(const Vec*)(in + b);
+        const f32x2* cs = turns + r * pairs + W * piece;
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            // pair j of the piece: elements j of u and of v, or 2 j and 2 j + 1 of the two together
+            T& ea = !PAIRS ? u.x[j] : 2 * j < W ? u.x[2 * j < W ? 2 * j : 0] : v.x[2 * j < W ? 0 : 2 * j - W];
+            T& eb = !PAIRS ? v.x[j] : 2 * j + 1 < W ? u.x[2 * j + 1 < W ? 2 * j + 1 : 0] : v.x[2 * j + 1 < W ? 0 : 2 * j + 1 - W];
+            const float fa = widened<T>(ea), fb = widened<T>(eb);
+            ea = narrowed<T>(fa * cs[j].x - fb * cs[j].y);
+            eb = narrowed<T>(fb * cs[j].x + fa * cs[j].y);
+        }
+        *(Vec*)(out + a) = u;
+        *(Vec*)(out + b) = v;
+    }
+}
+
+}  // namespace
+
+hipError_t launch_rotate_rows(const RotaryArgs& args, RotaryCall call, bool f32, hipStream_t st) {
+    if (call.n_rows <= 0) return hipSuccess;
+    const int e = f32 ? 4 : 2, w = 16 / e;
+    auto wide = [&](const RotaryRows& x) {
+        return x.n_heads == 0 || ((((uintptr_t)x.in | (uintptr_t)x.out) & 15) == 0 && x.in_stride % w == 0 && x.out_stride % w == 0);
+    };
+    const bool vec = call.rotary_dim % (2 * w) == 0 && call.head_dim % (2 * w) == 0 && wide(call.q) && wide(call.k);
+    // Rows per workgroup: enough workgroups for the chip first, then rows that keep all threads at sines and cosines.
+    call.rows_per_wg = call.n_rows >= 2048 ? 4 : call.n_rows >= 1024 ? 2 : 1;
+    const int64_t grid = (call.n_rows + call.rows_per_wg - 1) / call.rows_per_wg;
+    if (grid > 0x7fffffff) return hipErrorInvalidValue;
+    const size_t lds = (size_t)call.rows_per_wg * (call.rotary_dim / 2) * sizeof(f32x2);
+#define APAR_ROTATE(TV, WV, PV) hipLaunchKernelGGL((rotate_rows<TV, WV, PV>), dim3((unsigned)grid), dim3(256), lds, st, args, call)
+#define APAR_ROTATE_PAIRS(TV, WV)                 \
+    do {                                          \
+        if (call.pairs) APAR_ROTATE(TV, WV, true); \
+        else APAR_ROTATE(TV, WV, false);          \
+    } while (0)
+    if (f32) {
+        if (vec) APAR_ROTATE_PAIRS(float, 4);
+        else APAR_ROTATE_PAIRS(float, 1);
+    } else {
+        if (vec) APAR_ROTATE_PAIRS(uint16_t, 8);
+        else APAR_ROTATE_PAIRS(uint16_t, 1);
+    }
+#undef APAR_ROTATE_PAIRS
+#undef APAR_ROTATE
+    return hipGetLastError();
+}
+
+}  // namespace apar

@@ -204,7 +204,7 @@ def test_ragged_trees_every_block_boundary(chunk):
     assert run(manual_tree(parents, segs, HeadConfig(4, 4, 128, F4), seed=11), chunk=chunk).n_threads == 9
 
 
-@pytest.mark.parametrize("name,n_req,scale", [("mha64", 4, 1.0), ("ht256", 16, None), ("ht256", 6, 1.0), ("gqa1024", 2, 1.0)])
+@pytest.mark.parametrize("name,n_req,scale", [("mha64", 4, 1.0), ("ht256", 6, 1.0), ("gqa1024", 2, 1.0)])
 def test_config_shaped_subsets(name, n_req, scale):
     w = make_config(name, n_requests=n_req, data_scale=scale)
     w = type(w)(**{**w.__dict__, "heads": HeadConfig(w.heads.n_q_heads, w.heads.n_kv_heads, 128, F4)})

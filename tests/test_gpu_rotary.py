@@ -1,0 +1,239 @@
+"""Rotary positions against the definition in 64 bits (GPU only).
+
+Bounds from the roundings: the fraction of a turn is off by at most 2^-26 in 32 bits (9.4e-8 of angle), sine and cosine by two units of
+2^-24, the factor on both, two products and a sum round by 2^-24 each: together less than 2^-21 of s (|x_a| + |x_b|).  On bf16
+the result is rounded once more, by at most 2^-8 of it."""
+import numpy as np
+import pytest
+
+import paper_2401_06761_amd as ap
+
+pytestmark = pytest.mark.gpu
+
+
+def torch():
+    import torch as t
+
+    return t
+
+
+def wanted(x, positions, theta, magnitude, r, layout, transposed):
+    x = x.astype(np.float64)
+    angle = np.asarray(positions, dtype=np.float64)[:, None, None] * np.asarray(theta)
+    c, s = magnitude * np.cos(angle), magnitude * np.sin(angle) * (-1 if transposed else 1)
+    y, room = x.copy(), np.zeros_like(x)
+    ia = np.arange(r // 2) if layout == "half" else np.arange(0, r, 2)
+    ib = ia + r // 2 if layout == "half" else ia + 1
+    a, b = x[..., ia], x[..., ib]
+    y[..., ia], y[..., ib] = a * c - b * s, b * c + a * s
+    room[..., ia] = room[..., ib] = magnitude * (np.abs(a) + np.abs(b))
+    return y, room
+
+
+def check(got, x, positions, rot, transposed=False):
+    cfg = rot.cfg
+    layout = "half" if cfg.layout == ap.APAR_ROTARY_HALF else "pairs"
+    bf16 = got.dtype == torch().bfloat16
+    want, room = wanted(x.float().cpu().numpy(), positions, ap.apar_rotary_frequencies(rot.handle), cfg.magnitude, cfg.rotary_dim, layout, transposed)
+    off = np.abs(got.float().cpu().numpy().astype(np.float64) - want) - 2.0 ** -21 * room - (1.01 * 2.0 ** -8 * np.abs(want) if bf16 else 0)
+    rest = slice(cfg.rotary_dim, None)
+    assert np.array_equal(got[..., rest].float().cpu().numpy(), x[..., rest].float().cpu().numpy())
+    assert off[..., :cfg.rotary_dim].max() <= 0, off.max()
+
+
+def draw(rng, shape, dtype):
+    t = torch()
+    x = t.from_numpy(rng.standard_normal(shape).astype(np.float32)).cuda()
+    return x.to(t.bfloat16) if dtype == "bf16" else x
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+@pytest.mark.parametrize("n,hq,hkv,d,r", [(1, 1, 1, 128, 128), (3, 32, 8, 128, 64), (257, 5, 1, 64, 64), (2049, 3, 2, 128, 96), (1025, 2, 1, 256, 256),
+                                          (9, 3, 2, 80, 20), (5, 2, 2, 6, 2), (17, 4, 1, 128, 32), (33, 1, 3, 10, 10)])
+def test_rows_at_given_positions(dtype, layout, n, hq, hkv, d, r):
+    t = torch()
+    rng = np.random.default_rng(n * d + r)
+    pos = rng.integers(0, 1 << 20, n).astype(np.int32)
+    pos[0] = 0
+    p = t.from_numpy(pos).cuda()
+    with ap.Rotary(d, r, layout=layout, base=10000.0, scaling="ramp", factor=4.0, original_len=2048, magnitude=1.25) as rot:
+        for transposed in (False, True):
+            q, k = draw(rng, (n, hq, d), dtype), draw(rng, (n, hkv, d), dtype)
+            q0, k0 = q.clone(), k.clone()
+            qo, ko = t.full_like(q, 7.0), t.full_like(k, 7.0)
+            ap.apar_rotate_rows(rot.handle, p, q, k, qo, ko, transposed=transposed)
+            assert t.equal(q, q0) and t.equal(k, k0)
+            check(qo, q, pos, rot, transposed)
+            check(ko, k, pos, rot, transposed)
+            ap.apar_rotate_rows(rot.handle, p, q, k, transposed=transposed)  # in place
+            assert t.equal(q, qo) and t.equal(k, ko)
+            only = k0.clone()
+            ap.apar_rotate_rows(rot.handle, p, only, transposed=transposed)
+            assert t.equal(only, ko)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_of_a_wider_projection_and_unaligned_ones(dtype):
+    t = torch()
+    rng = np.random.default_rng(4)
+    pos = t.arange(40, dtype=t.int32, device="cuda") * 1000 - 5
+    with ap.Rotary(128, layout="half") as rot:
+        qkv = draw(rng, (40, 12, 128), dtype)
+        before = qkv.clone()
+        ap.apar_rotate_rows(rot.handle, pos, qkv[:, :8], qkv[:, 8:10])
+        check(qkv[:, :10], before[:, :10], pos.cpu().numpy(), rot)
+        assert t.equal(qkv[:, 10:], before[:, 10:])
+        for shift, step in ((1, 1024), (3, 1027), (0, 1025)):  # neither base nor rows on 16 bytes
+            flat = draw(rng, (40 * 1100,), dtype)
+            x = flat.as_strided((40, 8, 128), (step, 128, 1), shift)
+            old, was = x.clone(), flat.clone()
+            out = t.empty(40, 8, 128, dtype=x.dtype, device="cuda")
+            ap.apar_rotate_rows(rot.handle, pos, x, None, out)
+            check(out, old, pos.cpu().numpy(), rot)
+            ap.apar_rotate_rows(rot.handle, pos, x)
+            assert t.equal(x, out)
+            touched = t.zeros_like(flat, dtype=t.bool)
+            touched.as_strided((40, 1024), (step, 1), shift)[:] = True
+            assert t.equal(flat[~touched], was[~touched])
+
+
+def test_far_and_negative_positions():
+    t = torch()
+    rng = np.random.default_rng(5)
+    pos = np.array([2 ** 31 - 1, 2 ** 31 - 2, 2 ** 30 + 1, -(2 ** 31), -1, -12345, 10 ** 9], dtype=np.int32)
+    for base, scaling in ((10000.0, "none"), (500000.0, "linear"), (10.0, "base")):
+        with ap.Rotary(128, base=base, scaling=scaling, factor=16.0) as rot:
+            x = draw(rng, (len(pos), 2, 128), "f32")
+            out = t.empty_like(x)
+            ap.apar_rotate_rows(rot.handle, t.from_numpy(pos).cuda(), x, None, out)
+            # 2^31 positions times an angle that is itself rounded to 53 bits: 2^31 * 2^-53 of a radian beside the bounds above
+            want, room = wanted(x.cpu().numpy(), pos, ap.apar_rotary_frequencies(rot.handle), 1.0, 128, "half", False)
+            assert (np.abs(out.cpu().numpy() - want) <= (2.0 ** -21 + 2.0 ** -20) * room).all()
+
+
+def test_transposed_is_the_gradient():
+    """<g, y(x + e) - y(x)> = <x-gradient, e>: y is linear in x, so differences in 64 bits of the definition are exact, and the transposed
+    call on g has to equal the definition's transposed matrix times g; and it takes a turn back."""
+    t = torch()
+    rng = np.random.default_rng(6)
+    pos = t.tensor([0, 3, 77, 100000], dtype=t.int32, device="cuda")
+    for layout in ("half", "pairs"):
+        with ap.Rotary(128, 96, layout=layout, magnitude=1.5) as rot:
+            theta = ap.apar_rotary_frequencies(rot.handle)
+            g = draw(rng, (4, 2, 128), "f32")
+            got = t.empty_like(g)
+            ap.apar_rotate_rows(rot.handle, pos, g, None, got, transposed=True)
+            gn = g.cpu().numpy().astype(np.float64)
+            e = np.eye(128)
+            want = np.empty_like(gn)
+            for i in range(128):  # column i of the matrix of each row
+                col, _ = wanted(np.broadcast_to(e[i], (4, 2, 128)), pos.cpu().numpy(), theta, 1.5, 96, layout, False)
+                want[..., i] = (col * gn).sum(-1)
+            assert np.abs(got.cpu().numpy() - want).max() <= 2.0 ** -21 * 1.5 * 2 * np.abs(gn).max()
+        with ap.Rotary(128, 96, layout=layout) as rot:
+            x = draw(rng, (4, 2, 128), "f32")
+            y = x.clone()
+            ap.apar_rotate_rows(rot.handle, pos, y)
+            ap.apar_rotate_rows(rot.handle, pos, y, transposed=True)
+            assert (y - x).abs().max() <= 2 * 2.0 ** -21 * 4 * x.abs().max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32", "bf16_fp4kv"])
+def test_rows_of_listed_threads(dtype):
+    t = torch()
+    rng = np.random.default_rng(8)
+    hq, hkv = 4, 2
+    rows = "f32" if dtype == "f32" else "bf16"
+    with ap.Pool(hq, hkv, 128, dtype, 256) as pool, ap.Rotary(128, 64) as rot:
+        h = pool.handle
+        lens, threads = [37, 1, 200, 16], []
+        for n in lens:
+            th = ap.apar_thread_create(h)
+            z = draw(rng, (n, hkv, 128), rows)
+            ap.apar_append_kv(h, th, z, z)
+            threads.append(th)
+        empty = ap.apar_thread_create(h)
+        length = dict(zip(threads, lens))
+        length[empty] = 0
+
+        def compare(listed, positions, **kw):
+            q, k = draw(rng, (len(positions), hq, 128), rows), draw(rng, (len(positions), hkv, 128), rows)
+            qo, ko = t.empty_like(q), t.empty_like(k)
+            ap.apar_rotate_threads(h, rot.handle, listed, q, k, qo, ko, **kw)
+            check(qo, q, positions, rot)
+            check(ko, k, positions, rot)
+
+        order = [threads[2], empty, threads[0], threads[3], threads[1]]
+        compare(order, [length[x] for x in order])
+        again = [threads[0], threads[2], threads[0], threads[0], threads[2]]
+        compare(again, [37, 200, 38, 39, 201])
+        compare([threads[1], threads[0], threads[1]], [1, 2, 3, 37, 38, 4], m=[3, 2, 1])
+        compare([threads[0], threads[1], threads[2]], [37, 38, 1, 2, 200, 201], m=[2, 2, 2])
+        compare([threads[0], empty, threads[2]], [37, 200, 201], m=[1, 0, 2])
+        compare([threads[0], threads[3], threads[0]], [35, 36] + list(range(16)) + [36], m=[2, 16, 1], where=ap.APAR_ROWS_LAST)
+        many = [threads[i % 4] for i in range(1500)]  # more than go along with the arguments
+        pos, ahead = [], {}
+        for x in many:
+            pos.append(length[x] + ahead.get(x, 0))
+            ahead[x] = ahead.get(x, 0) + 1
+        compare(many, pos)
+        ms = [int(x) for x in rng.integers(0, 4, 700)]
+        pos, ahead = [], {}
+        for x, mi in zip(many, ms):
+            pos += [length[x] + ahead.get(x, 0) + j for j in range(mi)]
+            ahead[x] = ahead.get(x, 0) + mi
+        compare(many[:700], pos, m=ms)
+        masks = np.array([[1, 3, 5, 11, 16], [1, 2, 4, 12, 28], [0xFF, 0xE1, 4, 8, 16]], dtype=np.uint8)  # bits past the fifth do not count
+        depth = [[0, 1, 1, 2, 0], [0, 0, 0, 1, 2], [4, 0, 0, 0, 0]]
+        at = [threads[0], threads[2], threads[0]]
+        compare(at, [length[x] + y for x, d in zip(at, depth) for y in d], mask=t.from_numpy(masks).cuda(), n_cand=5)
+
+
+def test_refusals_of_the_binding():
+    t = torch()
+    with ap.Rotary(128) as rot, ap.Pool(4, 2, 128, "bf16", 4) as pool:
+        p = t.zeros(3, dtype=t.int32, device="cuda")
+        x = t.zeros(3, 2, 128, device="cuda")
+        for bad in (lambda: ap.apar_rotate_rows(rot.handle, p.long(), x), lambda: ap.apar_rotate_rows(rot.handle, p[:2], x),
+                    lambda: ap.apar_rotate_rows(rot.handle, p, x.half()), lambda: ap.apar_rotate_rows(rot.handle, p, x, x.bfloat16()),
+                    lambda: ap.apar_rotate_rows(rot.handle, p, x.cpu()), lambda: ap.apar_rotate_rows(rot.handle, p, None),
+                    lambda: ap.apar_rotate_rows(rot.handle, p, x[..., ::2]), lambda: ap.apar_rotate_rows(rot.handle, p, x[:1].expand(3, 2, 128)),
+                    lambda: ap.apar_rotate_rows(rot.handle, p, x, None, x[:2]), lambda: ap.apar_rotate_rows(rot.handle, p.cpu(), x)):
+            with pytest.raises(ValueError):
+                bad()
+        th = ap.apar_thread_create(pool.handle)
+        y = t.zeros(1, 4, 128, dtype=t.bfloat16, device="cuda")
+        with pytest.raises(ap.AparError):
+            ap.apar_rotate_threads(pool.handle, rot.handle, [th], y[:, :2].contiguous())  # not the pool's heads
+        with pytest.raises(ap.AparError):
+            ap.apar_rotate_threads(pool.handle, rot.handle, [th], y.float())  # not the pool's type
+        with pytest.raises(ap.AparError):
+            ap.apar_rotate_threads(pool.handle, rot.handle, [th], y, n_cand=1)  # no mask
+        ap.apar_rotate_rows(rot.handle, p[:0], x[:0])  # nothing to do
+
+
+def test_on_a_stream_and_in_a_graph():
+    t = torch()
+    rng = np.random.default_rng(9)
+    with ap.Rotary(128) as rot:
+        x, pos = draw(rng, (64, 8, 128), "bf16"), t.arange(64, dtype=t.int32, device="cuda")
+        want = t.empty_like(x)
+        ap.apar_rotate_rows(rot.handle, pos, x, None, want)
+        s = t.cuda.Stream()
+        s.wait_stream(t.cuda.current_stream())
+        got = t.zeros_like(x)
+        with t.cuda.stream(s):
+            ap.apar_rotate_rows(rot.handle, pos, x, None, got)
+        s.synchronize()
+        assert t.equal(got, want)
+        g = t.cuda.CUDAGraph()
+        with t.cuda.graph(g):
+            ap.apar_rotate_rows(rot.handle, pos, x, None, got)
+        for step in range(3):
+            x.copy_(draw(rng, (64, 8, 128), "bf16"))
+            pos.add_(step)
+            g.replay()
+            ap.apar_rotate_rows(rot.handle, pos, x, None, want)
+            t.cuda.synchronize()
+            assert t.equal(got, want)
