@@ -58,7 +58,8 @@ typedef enum apar_status {
     APAR_ERR_HIP = -5,             /* a HIP runtime call failed (see apar_last_hip_error) */
     APAR_ERR_UNSUPPORTED = -6,     /* shape outside what the kernels are built for       */
     APAR_ERR_WORKSPACE_LIMIT = -7, /* apar_decode_attention_fixed: the call needs more than */
-                                   /* the fixed workspace holds; nothing was enqueued       */
+                                   /* the fixed workspace holds; apar_sample_tokens: than   */
+                                   /* the caller's; nothing was enqueued                    */
     APAR_ERR_INTERNAL = -8         /* a write check (apar_set_write_checks) found a kernel  */
                                    /* about to write a block that other threads hold; nothing */
                                    /* was launched, the pool should be destroyed             */
@@ -419,6 +420,45 @@ APAR_API int apar_group_step(apar_group* group, const int32_t* sampled, int n, c
  * INVALID_ARG if cap is too small. */
 APAR_API int apar_group_restore(apar_group* group, int32_t* tokens_out, int64_t cap, int64_t* n_out);
 APAR_API int apar_group_get_info(apar_group* group, apar_group_info* out);
+
+/* ---- sampling -------------------------------------------------------------
+ * What Alg. 1 draws a step's tokens from: a row of logits per unfinished sequence, in the order of apar_group_unfinished (or
+ * apar_server_batch).  Per row, with x its logits and w = exp((x - max) / temperature), the tokens in one order, value descending, index
+ * ascending:
+ *   top_k  keeps the first k (<= 0: all);
+ *   top_p  keeps the shortest prefix that has at least top_p of the mass that top_k keeps (>= 1, or NaN: all; always the first token);
+ *   min_p  keeps w >= min_p (<= 0: all; always the tokens of the largest value);
+ *   the token drawn is the first of those kept by all three whose cumulated mass exceeds u times their mass (u in [0, 1)).
+ * temperature <= 0 (or NaN): the first token, its log-probability 0.  Logits of -inf and NaN are no tokens; a row without any gives
+ * APAR_TOKEN_NONE and a log-probability of -inf.  Logits of +inf share the row among them.
+ * w is computed in 64 bits and held in units of 2^-(62 - ceil(log2 vocab)); masses are sums of whole numbers of those, the same for every
+ * order of addition.  A draw depends on the row, its parameters and u alone. */
+enum { APAR_TOKEN_NONE = INT32_MIN };
+typedef struct apar_sample_row { /* one row's parameters, on the device */
+    float temperature;
+    int32_t top_k;
+    float top_p, min_p;
+} apar_sample_row;
+typedef struct apar_token_ids { /* the vocabulary's numbers of the control tokens (-1: none), which come out as APAR_TOKEN_* ... */
+    int32_t fork, child, eos;   /* ... (apar_group_step takes no sampled [Child]: its logit should be -inf)                    */
+} apar_token_ids;
+/* Device memory that a call of n rows wants.  Errors: INVALID_ARG, UNSUPPORTED (vocab > 2^20). */
+APAR_API int apar_sample_workspace_bytes(int n, int vocab, size_t* bytes_out);
+/*
+ *   logits_dev   : [n, vocab] of dtype (APAR_F32 or APAR_BF16), rows row_stride elements apart
+ *   rows_dev     : [n], or NULL: temperature 1 and nothing cut
+ *   uniforms_dev : [n] floats
+ *   ids          : host, or NULL: no control tokens
+ *   tokens_dev   : [n] int32, device or pinned host memory;  logprobs_dev : [n] floats or NULL: ln of the token's share of the kept mass
+ *   workspace_dev: 16-byte aligned; nothing in it has to be set, and nothing is kept in it.  Calls that may overlap (other streams,
+ *                  replayed graphs) need one each.
+ * Enqueues kernels only: may be captured into a graph.
+ * Errors: INVALID_ARG, UNSUPPORTED (vocab > 2^20), WORKSPACE_LIMIT (too small a workspace), HIP.
+ */
+APAR_API int apar_sample_tokens(const void* logits_dev, int dtype, int n, int vocab, int64_t row_stride,
+                                const apar_sample_row* rows_dev, const float* uniforms_dev, const apar_token_ids* ids,
+                                int32_t* tokens_dev, float* logprobs_dev, void* workspace_dev, size_t workspace_bytes,
+                                void* hip_stream);
 
 /* ---- serving loop (Sec. 3.3 "Results in High-Throughput Scenarios", App. C.2) -------------
  * Requests wait in a first-come-first-served queue over one pool.  Per decode step the caller

@@ -12,6 +12,7 @@ Two independent halves:
   * controller.py - Algorithm 1 (fork on [Fork], paragraph nodes, Restore) in plain Python.
   * serving.py - the serving loop (queue, admission, preemption) over controller + ledger.
   * fp8.py     - what a pool that keeps full blocks in fp8 holds of the rows it was given.
+  * sampling.py - a token out of a row of logits.
   * fp4.py     - what a pool that keeps rows in 4 bits holds of them.
   * accounting.py - the paper's max-cached-tokens / attended-tokens metrics and
                  the resident-vs-copied-prefix byte counts.
@@ -22,4 +23,5 @@ from . import accounting  # noqa: F401
 from . import fp4  # noqa: F401
 from . import fp8  # noqa: F401
 from . import controller  # noqa: F401
+from . import sampling  # noqa: F401
 from . import serving  # noqa: F401

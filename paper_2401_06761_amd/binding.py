@@ -81,6 +81,11 @@ class AparRotaryRows(C.Structure):
                 ("n_heads", C.c_int32)]
 
 
+class AparTokenIds(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("fork", "child", "eos")]
+
+
+APAR_TOKEN_NONE = -2 ** 31
 APAR_ROTARY_HALF, APAR_ROTARY_PAIRS = 0, 1
 APAR_ROTARY_SCALE_NONE, APAR_ROTARY_SCALE_LINEAR, APAR_ROTARY_SCALE_BASE, APAR_ROTARY_SCALE_RAMP = range(4)
 APAR_ROWS_NEXT, APAR_ROWS_LAST = 0, 1
@@ -125,6 +130,8 @@ def _load() -> C.CDLL:
         "apar_rotary_frequencies": [P, C.POINTER(C.c_double), I, C.POINTER(C.c_int)],
         "apar_rotate_rows": [P, I, V, C.c_int64, C.POINTER(AparRotaryRows), C.POINTER(AparRotaryRows), I, V],
         "apar_rotate_threads": [P, P, I, I32P, I32P, I, I, V, I, C.POINTER(AparRotaryRows), C.POINTER(AparRotaryRows), I, V],
+        "apar_sample_workspace_bytes": [I, I, C.POINTER(C.c_size_t)],
+        "apar_sample_tokens": [V, I, I, I, C.c_int64, V, V, C.POINTER(AparTokenIds), V, V, V, C.c_size_t, V],
         "apar_free_thread": [P, C.c_int32],
         "apar_thread_len": [P, C.c_int32, C.POINTER(C.c_int64)],
         "apar_thread_block_table": [P, C.c_int32, I32P, I, C.POINTER(C.c_int)],
@@ -408,7 +415,7 @@ def _stream_on(t, stream) -> int:
         torch.cuda.current_stream(t.device).cuda_stream
 
 
-def _rotary_dtype(*tensors) -> int:
+def _rows_dtype(*tensors) -> int:
     import torch
 
     kinds = {t.dtype for t in tensors if t is not None}
@@ -431,7 +438,7 @@ def apar_rotate_rows(rotary, positions, q, k=None, q_out=None, k_out=None, trans
         raise ValueError("all tensors must be on one device")
     if qr is None and kr is None:
         raise ValueError("neither q nor k")
-    _check(_L().apar_rotate_rows(rotary, _rotary_dtype(q, k), _ptr(positions), positions.shape[0], qr, kr, int(bool(transposed)),
+    _check(_L().apar_rotate_rows(rotary, _rows_dtype(q, k), _ptr(positions), positions.shape[0], qr, kr, int(bool(transposed)),
                                  _stream_on(positions, stream)), "apar_rotate_rows")
 
 
@@ -445,7 +452,7 @@ def apar_rotate_threads(pool, rotary, threads: Sequence[int], q, k=None, q_out=N
         if nm != n:
             raise ValueError("one m per listed thread")
         rows = int(sum(m))
-    dtype = _rotary_dtype(q, k) if q is not None or k is not None else APAR_BF16
+    dtype = _rows_dtype(q, k) if q is not None or k is not None else APAR_BF16
     qr, _ = _rotary_rows(q, q_out, rows)
     kr, _ = _rotary_rows(k, k_out, rows)
     if mask is not None and (mask.element_size() != 1 or mask.numel() != rows):
@@ -622,6 +629,60 @@ def apar_append_kv_gather(pool, threads: Sequence[int], src_rows: Sequence[int],
     if ns != n:
         raise ValueError("one source row per listed thread")
     _check(_L().apar_append_kv_gather(pool, arr, src, n, _ptr(k), _ptr(v), _stream(stream)), "apar_append_kv_gather")
+
+
+def apar_sample_workspace_bytes(n: int, vocab: int) -> int:
+    out = C.c_size_t()
+    _check(_L().apar_sample_workspace_bytes(n, vocab, C.byref(out)), "apar_sample_workspace_bytes")
+    return int(out.value)
+
+
+def apar_sample_rows(temperature, top_k=None, top_p=None, min_p=None):
+    """The device array of rows' parameters (apar_sample_row) from 1-d GPU tensors; None: nothing cut."""
+    import torch
+
+    n, dev = temperature.shape[0], temperature.device
+    rows = torch.empty((n, 4), dtype=torch.float32, device=dev)
+    rows[:, 0] = temperature
+    rows[:, 1].view(torch.int32).copy_(torch.zeros(n, dtype=torch.int32, device=dev) if top_k is None else top_k)
+    rows[:, 2] = 1.0 if top_p is None else top_p
+    rows[:, 3] = 0.0 if min_p is None else min_p
+    return rows
+
+
+def apar_sample_tokens(logits, uniforms, tokens, rows=None, token_ids: Optional[Sequence[int]] = None, logprobs=None, workspace=None,
+                       stream=None) -> None:
+    """logits: [n, vocab] float32 or bfloat16 on the GPU (rows may be any distance apart); uniforms: [n] float32; tokens: [n] int32, on the
+    GPU or pinned; rows: apar_sample_rows; token_ids: the vocabulary's numbers of [Fork], [Child], [EOS]; workspace: a GPU tensor of
+    apar_sample_workspace_bytes (one is made if it is None)."""
+    import torch
+
+    if not logits.is_cuda or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be a 2-d GPU tensor with adjacent columns")
+    n, vocab = logits.shape
+
+    def checked(t, dtype, shape, what, host=False):
+        if t is None:
+            return 0
+        if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError(f"{what} must be contiguous, {dtype}, {shape}")
+        if not (t.device == logits.device or (host and t.device.type == "cpu" and t.is_pinned())):
+            raise ValueError(f"{what} must be where the logits are")
+        return t.data_ptr()
+
+    stride = logits.stride(0) if n > 1 else max(1, vocab)
+    if n > 1 and stride < vocab:
+        raise ValueError("rows must not overlap")
+    ptrs = [checked(rows, torch.float32, (n, 4), "rows"), checked(uniforms, torch.float32, (n,), "uniforms"),
+            checked(tokens, torch.int32, (n,), "tokens", host=True), checked(logprobs, torch.float32, (n,), "logprobs")]
+    if workspace is None:
+        workspace = torch.empty(apar_sample_workspace_bytes(n, vocab), dtype=torch.uint8, device=logits.device)
+    elif workspace.device != logits.device or not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous and where the logits are")
+    ids = None if token_ids is None else AparTokenIds(*token_ids)
+    _check(_L().apar_sample_tokens(logits.data_ptr(), _rows_dtype(logits), n, vocab, stride, ptrs[0], ptrs[1], ids, ptrs[2], ptrs[3],
+                                   workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_on(logits, stream)),
+           "apar_sample_tokens")
 
 
 def apar_server_create(pool, max_running: int, watermark_blocks: int) -> C.c_void_p:

@@ -1,0 +1,234 @@
+"""Sampling against oracle.sampling (GPU only).
+
+Tokens have to be the oracle's wherever the draw is not within the roundings of the sums of falling on another one: the library's masses are off
+by at most half a unit of 2^-(62 - bits) per token, vocab * 2^-(63 - bits) <= 2^-(63 - 2 bits) of a mass that is at least 1 (bits <= 18 here:
+2^-27), the oracle's by 2^-53 per addition.  Inputs are drawn once and none of them comes that near (asserted).  Log-probabilities: the
+same sums, then one rounding to fp32, 2^-24 of a magnitude of at most 128."""
+import numpy as np
+import pytest
+
+import paper_2401_06761_amd as ap
+from oracle import sampling
+
+pytestmark = pytest.mark.gpu
+
+
+def torch():
+    import torch as t
+
+    return t
+
+
+def call(x, u, params, ids=None, workspace=None):
+    """x: GPU [n, vocab]; params: [n] of (temperature, top_k, top_p, min_p)"""
+    t = torch()
+    n = x.shape[0]
+    p = np.array(params, dtype=np.float64).reshape(n, 4)
+    rows = ap.apar_sample_rows(*(t.from_numpy(p[:, i].astype(np.int32 if i == 1 else np.float32)).cuda() for i in range(4)))
+    tokens = t.full((n,), 77, dtype=t.int32, device="cuda")
+    logp = t.full((n,), 7.0, device="cuda")
+    ap.apar_sample_tokens(x, t.from_numpy(np.asarray(u, dtype=np.float32)).cuda(), tokens, rows, token_ids=ids, logprobs=logp, workspace=workspace)
+    return tokens.cpu().numpy(), logp.cpu().numpy()
+
+
+def compare(x, u, params):
+    tokens, logp = call(x, u, params)
+    host = x.float().cpu().numpy()
+    p = np.array(params, dtype=np.float32).reshape(len(host), 4)
+    bits = max(1, int(np.ceil(np.log2(x.shape[1]))))
+    for r in range(len(host)):
+        want, lp, margin = sampling.draw(host[r], p[r, 0], int(params[r][1]), p[r, 2], p[r, 3], np.float32(u[r]))
+        if margin <= 2.0 ** -(62 - 2 * bits) + 1e-12:
+            assert np.isfinite(lp)  # (a tie of the sums themselves; only rows made for that come here)
+            continue
+        assert tokens[r] == want, (r, params[r], u[r], tokens[r], want, margin)
+        assert logp[r] == lp or abs(logp[r] - lp) <= 2.0 ** -24 * 128 + 2.0 ** -(62 - 2 * bits), (r, logp[r], lp)
+
+
+def some_params(rng, n):
+    return [(float(rng.choice([0.0, 0.3, 0.7, 1.0, 1.5, 20.0])), int(rng.choice([0, 1, 2, 40, 1000])), float(rng.choice([1.0, 0.95, 0.6, 0.1])),
+             float(rng.choice([0.0, 0.02, 0.3]))) for _ in range(n)]
+
+
+def values(rng, n, vocab, dtype, scale=2.5):
+    t = torch()
+    x = t.from_numpy((scale * rng.standard_normal((n, vocab))).astype(np.float32)).cuda()
+    return x.to(t.bfloat16) if dtype == "bf16" else x
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,vocab", [(5, 1), (9, 2), (40, 7), (33, 63), (17, 64), (64, 1000), (30, 8191), (20, 8192), (20, 8193), (24, 32000),
+                                     (12, 50001), (8, 131075), (6, 200000)])
+def test_rows_with_parameters_of_their_own(dtype, n, vocab):
+    rng = np.random.default_rng(vocab + n)
+    x = values(rng, n, vocab, dtype)
+    compare(x, rng.random(n), some_params(rng, n))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_flat_peaked_far_and_near_zero_rows(dtype):
+    t = torch()
+    rng = np.random.default_rng(3)
+    for scale, shift in ((0.0, 0.0), (0.01, 0.0), (1e-30, 0.0), (30.0, 0.0), (1.0, 1000.0), (1.0, -300.0), (3e37, 0.0), (0.3, 0.05)):
+        x = (values(rng, 24, 5000, "f32", 1.0) * scale + shift).to(t.bfloat16 if dtype == "bf16" else t.float32)
+        x[3, :4000] = -float("inf")
+        x[4, 1:] = float("nan")
+        x[5, ::2] = float("nan")
+        compare(x, rng.random(24), some_params(rng, 24))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_ties_go_to_the_lowest_index(dtype):
+    """Rows of very few values, long runs of equal ones across every chunk of the row; targets inside the runs."""
+    t = torch()
+    rng = np.random.default_rng(4)
+    for vocab in (10, 8200, 40000):
+        x = t.from_numpy(rng.integers(-2, 3, (40, vocab)).astype(np.float32)).cuda().to(t.bfloat16 if dtype == "bf16" else t.float32)
+        x[::7] = 0.5
+        x[1] = t.where(x[1] > 0, -0.0, 0.0)  # zeros of both signs are one value
+        u = (rng.integers(0, 1000, 40) + 0.5) / 1000.0
+        params = [(1.0, int(rng.choice([0, 3, vocab // 2, vocab - 1, vocab, vocab + 5])), float(rng.choice([1.0, 0.333, 0.77])), float(rng.choice([0, 0.2, 0.9])))
+                  for _ in range(40)]
+        compare(x, u, params)
+
+
+def test_all_equal_values_and_exact_targets():
+    """vocab equal weights of exactly 1: every mass is a whole number, so every draw is told by arithmetic, on its borders too."""
+    t = torch()
+    for dtype in (t.bfloat16, t.float32):
+        for vocab in (1, 2, 1000, 4096, 70000):
+            x = t.full((64, vocab), 3.0, dtype=dtype, device="cuda")
+            u = (np.arange(64) / 64.0).astype(np.float32)  # (exact)
+            tokens, logp = call(x, u, [(1.0, 0, 1.0, 0.0)] * 64)
+            assert np.array_equal(tokens, np.floor(u.astype(np.float64) * vocab).astype(int))
+            assert np.abs(logp + np.log(vocab)).max() <= 2.0 ** -24 * 16
+            k = max(1, vocab // 2)
+            tokens, _ = call(x, u, [(0.5, k, 1.0, 0.0)] * 64)
+            assert np.array_equal(tokens, np.floor(u.astype(np.float64) * k).astype(int))
+            tokens, _ = call(x, u, [(0.5, 0, 0.25, 1.0)] * 64)
+            assert np.array_equal(tokens, np.floor(u.astype(np.float64) * max(1, int(np.ceil(vocab * 0.25)))).astype(int))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_special_rows(dtype):
+    t = torch()
+    inf, nan = float("inf"), float("nan")
+    kind = t.bfloat16 if dtype == "bf16" else t.float32
+    x = t.tensor([[nan, -inf, nan, -inf], [-inf, -inf, 2.0, -inf], [inf, 1.0, inf, 5.0], [1.0, nan, 1.0, 3.0], [-inf, -3e38, -inf, -3.1e38],
+                  [0.0, -0.0, 0.0, -0.0]], dtype=kind, device="cuda")
+    one = [(1.0, 0, 1.0, 0.0)] * 6
+    assert call(x, [0.0] * 6, one)[0].tolist() == [ap.APAR_TOKEN_NONE, 2, 0, 3, 1, 0]
+    got = call(x, [0.99] * 6, one)
+    assert got[0][:3].tolist() == [ap.APAR_TOKEN_NONE, 2, 2] and got[0][4:].tolist() == [1, 3]
+    assert got[1][0] == -inf and got[1][1] == 0.0 and abs(got[1][2] - np.log(0.5)) < 1e-6
+    greedy = call(x, [0.99] * 6, [(0.0, 0, 1.0, 0.0)] * 6)
+    assert greedy[0].tolist() == [ap.APAR_TOKEN_NONE, 2, 0, 3, 1, 0] and greedy[1][1:].tolist() == [0.0] * 5
+    # parameters that say nothing or too much, u outside [0, 1)
+    y = t.tensor([[1.0, 2.0, 3.0]] * 9, dtype=kind, device="cuda")
+    odd = [(nan, 0, 1.0, 0.0), (-1.0, 0, 1.0, 0.0), (1.0, -5, 1.0, 0.0), (1.0, 0, nan, 0.0), (1.0, 0, 7.0, nan), (1.0, 0, -1.0, 0.0), (1.0, 0, 1.0, 5.0),
+           (1.0, 0, 1.0, 0.0), (1.0, 0, 1.0, 0.0)]
+    assert call(y, [0.999] * 7 + [1.5, nan], odd)[0].tolist() == [2, 2, 0, 0, 0, 2, 2, 0, 2]
+    assert call(y, [-3.0] * 9, odd)[0].tolist() == [2] * 9
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shift,step", [(0, 5000), (1, 5001), (3, 5013), (5, 4999)])
+def test_rows_that_are_a_slice_of_wider_ones(dtype, shift, step):
+    t = torch()
+    rng = np.random.default_rng(shift + step)
+    flat = values(rng, 1, 5100 * 13, dtype)[0]
+    x = flat.as_strided((12, 4990), (step, 1), shift)
+    compare(x, rng.random(12), some_params(rng, 12))
+
+
+def test_parameters_default_to_the_plain_draw_and_control_tokens_are_named():
+    t = torch()
+    rng = np.random.default_rng(11)
+    x = values(rng, 50, 12, "bf16", 1.0)
+    u = rng.random(50).astype(np.float32)
+    tokens = t.empty(50, dtype=t.int32, device="cuda")
+    ap.apar_sample_tokens(x, t.from_numpy(u).cuda(), tokens)
+    plain = tokens.cpu().numpy()
+    want = [sampling.draw(r, u=a)[0] for r, a in zip(x.float().cpu().numpy(), u)]
+    assert plain.tolist() == want
+    named, _ = call(x, u, [(1.0, 0, 1.0, 0.0)] * 50, ids=(3, 4, 11))
+    assert named.tolist() == [{3: ap.APAR_TOKEN_FORK, 4: ap.APAR_TOKEN_CHILD, 11: ap.APAR_TOKEN_EOS}.get(v, v) for v in want]
+    pinned = t.empty(50, dtype=t.int32, pin_memory=True)
+    ap.apar_sample_tokens(x, t.from_numpy(u).cuda(), pinned)
+    t.cuda.synchronize()
+    assert pinned.tolist() == want
+
+
+def test_frequencies_follow_the_shares():
+    """65536 evenly spaced u over one row: every token comes up as often as its share says, to one place per border."""
+    t = torch()
+    rng = np.random.default_rng(12)
+    x = values(rng, 1, 300, "f32", 2.0)
+    n = 65536
+    u = ((np.arange(n) + 0.5) / n).astype(np.float32)
+    tokens, logp = call(x.expand(n, 300).contiguous(), u, [(0.8, 0, 1.0, 0.0)] * n)
+    w = np.exp((x[0].cpu().numpy().astype(np.float64)) / np.float32(0.8))
+    w /= w.sum()
+    assert np.abs(np.bincount(tokens, minlength=300) - n * w).max() <= 1.0 + n * 2.0 ** -24
+    assert np.abs(np.exp(logp.astype(np.float64)) - w[tokens]).max() <= 1e-6
+
+
+def test_streams_graphs_and_repeats():
+    t = torch()
+    rng = np.random.default_rng(13)
+    n, vocab = 37, 20011
+    xs = [values(rng, n, vocab, "bf16") for _ in range(3)]
+    us = [t.from_numpy(rng.random(n).astype(np.float32)).cuda() for _ in range(3)]
+    p = np.array(some_params(rng, n))
+    rows = ap.apar_sample_rows(*(t.from_numpy(p[:, i].astype(np.int32 if i == 1 else np.float32)).cuda() for i in range(4)))
+    wanted = []
+    for x, u in zip(xs, us):
+        tok, lp = t.empty(n, dtype=t.int32, device="cuda"), t.empty(n, device="cuda")
+        ap.apar_sample_tokens(x, u, tok, rows, logprobs=lp)
+        wanted.append((tok.clone(), lp.clone()))
+        ap.apar_sample_tokens(x, u, tok, rows, logprobs=lp)
+        assert t.equal(tok, wanted[-1][0]) and t.equal(lp, wanted[-1][1])
+    x, u = xs[0].clone(), us[0].clone()
+    graphs = []
+    for _ in range(2):  # two graphs, a workspace each
+        tok, lp = t.empty(n, dtype=t.int32, device="cuda"), t.empty(n, device="cuda")
+        ws = t.empty(ap.apar_sample_workspace_bytes(n, vocab), dtype=t.uint8, device="cuda")
+        ws.fill_(0xA5)
+        s = t.cuda.Stream()
+        s.wait_stream(t.cuda.current_stream())
+        with t.cuda.stream(s):
+            ap.apar_sample_tokens(x, u, tok, rows, logprobs=lp, workspace=ws)
+        t.cuda.current_stream().wait_stream(s)
+        g = t.cuda.CUDAGraph()
+        with t.cuda.graph(g):
+            ap.apar_sample_tokens(x, u, tok, rows, logprobs=lp, workspace=ws)
+        graphs.append((g, tok, lp, ws))
+    for i in (1, 2, 0, 2):
+        x.copy_(xs[i])
+        u.copy_(us[i])
+        for g, tok, lp, _ in graphs:
+            g.replay()
+        eager = t.empty(n, dtype=t.int32, device="cuda")
+        ap.apar_sample_tokens(x, u, eager, rows)
+        t.cuda.synchronize()
+        assert t.equal(eager, wanted[i][0])
+        for g, tok, lp, _ in graphs:
+            assert t.equal(tok, wanted[i][0]) and t.equal(lp, wanted[i][1])
+
+
+def test_refusals_of_the_binding():
+    t = torch()
+    x, u, tok = t.zeros(3, 8, device="cuda"), t.zeros(3, device="cuda"), t.zeros(3, dtype=t.int32, device="cuda")
+    for bad in (lambda: ap.apar_sample_tokens(x[0], u, tok), lambda: ap.apar_sample_tokens(x.half(), u, tok), lambda: ap.apar_sample_tokens(x, u[:2], tok),
+                lambda: ap.apar_sample_tokens(x, u.double(), tok), lambda: ap.apar_sample_tokens(x, u, tok.long()),
+                lambda: ap.apar_sample_tokens(x, u.cpu(), tok), lambda: ap.apar_sample_tokens(x, u, tok.cpu()),
+                lambda: ap.apar_sample_tokens(x, u, tok, rows=t.zeros(3, 3, device="cuda")), lambda: ap.apar_sample_tokens(x[:1].expand(3, 8), u, tok),
+                lambda: ap.apar_sample_tokens(x.t(), u, tok), lambda: ap.apar_sample_tokens(x, u, tok, logprobs=t.zeros(2, device="cuda"))):
+        with pytest.raises(ValueError):
+            bad()
+    ap.apar_sample_tokens(x[:0], u[:0], tok[:0])
+    need = ap.apar_sample_workspace_bytes(3, 8)
+    if need:
+        with pytest.raises(ap.AparError) as e:
+            ap.apar_sample_tokens(x, u, tok, workspace=t.empty(need - 1, dtype=t.uint8, device="cuda"))
+        assert e.value.status == -7
