@@ -6,8 +6,15 @@
 // is the place where a cumulated count or mass reaches a target, found by digits of the values' ordered bit patterns (keys), 12, 12 and
 // 8 bits: a histogram of counts and masses over the first digit, then over the next one of the values that share the first, and so
 // on; among equal values the place follows from their weight, and the index from counting them.
-// Masses are sums of whole numbers, w 2^weight_bits rounded (42 to 61 bits by the size of the vocabulary, w computed in 64): they
+// Masses are sums of whole numbers, w 2^weight_bits rounded (42 to 62 bits by the size of the vocabulary, w computed in 64): they
 // do not depend on the order of the additions, and all prefixes agree with each other.
+//
+// bf16 rows (sample_rows_bf16): there are 65536 values, and a workgroup has room to count each of them (128 KiB of LDS, two counters to a
+// word).  A weight is then worked out once per value and not once per token (tens of vector instructions in 64 bits): per run
+// of 64 values that occur at all, by a wavefront each, to a count and a mass; and every target is reached by one wavefront, first among those
+// runs, then among the 64 values of one.  The row stays in registers for the pass that looks for the token's index.  A value
+// that occurs more than 65535 times shows in the counters' sum; such a row goes through the digits.  Both ways give the same token.
+// What bounds it: memory, behind that the passes over the counters, which nothing fills where a compute unit has one row.
 #include <hip/hip_runtime.h>
 
 #include "apar_internal.hpp"
@@ -123,13 +130,43 @@ __device__ __forceinline__ int reach(Shared& s, const uint32_t* counts, const u6
     return bin;
 }
 
+// A token's number as the caller wants it.
+__device__ __forceinline__ void write_token(const SampleCall& call, int r, int index) {
+    call.tokens[r] = index == call.ids.fork ? APAR_TOKEN_FORK : index == call.ids.child ? APAR_TOKEN_CHILD
+                     : index == call.ids.eos ? APAR_TOKEN_EOS : index;
+}
+__device__ __forceinline__ void write_none(const SampleCall& call, int r) {
+    call.tokens[r] = APAR_TOKEN_NONE;
+    if (call.logprobs) call.logprobs[r] = -INFINITY;
+}
+
+// A row's weights: w = exp((x - max) / T), and in whole units.
+struct Weights {
+    double top, temperature, one;
+    __device__ __forceinline__ double of(float x) const { return (double)x == top ? 1.0 : exp(((double)x - top) / temperature); }
+    __device__ __forceinline__ u64 whole(double w) const { return (u64)(w * one + 0.5); }
+    __device__ __forceinline__ u64 units(float x) const { return whole(of(x)); }
+    __device__ __forceinline__ float logprob(float x, u64 mass) const {
+        const double z = (double)x == top ? 0.0 : ((double)x - top) / temperature;
+        return (float)(z - log((double)mass / one));
+    }
+};
+__device__ __forceinline__ double unit_of(const SampleCall& call) { return (double)(1ull << call.weight_bits); }
+
+// Targets that the cuts and the draw set.
+__device__ __forceinline__ u64 top_p_target(float top_p, u64 mass) {
+    return max((u64)1, min((u64)ceil((double)fmaxf(top_p, 0.0f) * (double)mass), mass));
+}
+__device__ __forceinline__ u64 draw_target(float u, u64 mass) {  // the first prefix of more than u times the mass
+    return min((u64)((double)fminf(fmaxf(u, 0.0f), 1.0f) * (double)mass) + 1, mass);
+}
+
+// By digits, any type and size.
 template <class T>
-__global__ __launch_bounds__(kThreads) void sample_rows(SampleCall call) {
-    __shared__ Shared s;
-    const int r = blockIdx.x, vocab = call.vocab;
+__device__ void sample_by_digits(Shared& s, const SampleCall& call, int r) {
+    const int vocab = call.vocab;
     const T* row = (const T*)call.logits + (int64_t)r * call.row_stride;
     const apar_sample_row p = call.rows ? call.rows[r] : apar_sample_row{1.0f, 0, 1.0f, 0.0f};
-    const double one = ldexp(1.0, call.weight_bits);
     const bool greedy = !(p.temperature > 0.0f);
 
     for (int i = threadIdx.x; i < kBins; i += kThreads) s.count0[i] = 0, s.mass0[i] = 0;
@@ -145,31 +182,26 @@ __global__ __launch_bounds__(kThreads) void sample_rows(SampleCall call) {
     __syncthreads();
     top = s.top;
     if (top == 0) {  // nothing but -inf and NaN
-        if (threadIdx.x == 0) {
-            call.tokens[r] = APAR_TOKEN_NONE;
-            if (call.logprobs) call.logprobs[r] = -INFINITY;
-        }
+        if (threadIdx.x == 0) write_none(call, r);
         return;
     }
-    const double x_top = value_of(top);
-    const double temperature = p.temperature;
-    auto weight = [&](float x) -> double { return (double)x == x_top ? 1.0 : exp(((double)x - x_top) / temperature); };
-    auto whole = [&](double w) -> u64 { return (u64)(w * one + 0.5); };
+    const Weights weights{value_of(top), p.temperature, unit_of(call)};
 
     Found token{top, 0, 0, 0};
-    u64 kept_mass = whole(1.0);
+    u64 kept_mass = 0;
     if (!greedy) {
+        const double least = p.min_p > 0.0f ? fmin((double)p.min_p, 1.0) : 0.0;
         uint32_t n = 0, n_min = 0;
         u64 m = 0, m_min = 0;
         each<T>(row, vocab, [&](int, float x) {
             if (!(x > -INFINITY)) return;
             const uint32_t key = key_of(x);
-            const double wd = weight(x);
-            const u64 w = whole(wd);
+            const double wd = weights.of(x);
+            const u64 w = weights.whole(wd);
             atomicAdd(&s.count0[key >> 20], 1u);
             atomicAdd(&s.mass0[key >> 20], w);
             n += 1, m += w;
-            if (!(wd < (double)p.min_p) || key == top) n_min += 1, m_min += w;
+            if (!(wd < least)) n_min += 1, m_min += w;
         });
         atomicAdd(&s.total_count, n);
         atomicAdd(&s.total_mass, m);
@@ -191,18 +223,18 @@ __global__ __launch_bounds__(kThreads) void sample_rows(SampleCall call) {
                     const uint32_t key = key_of(x);
                     if (!(x > -INFINITY) || key >> (shift + (digit == 1 ? 12 : 8)) != prefix) return;
                     atomicAdd(&s.count1[(key >> shift) & (bins - 1)], 1u);
-                    atomicAdd(&s.mass1[(key >> shift) & (bins - 1)], whole(weight(x)));
+                    atomicAdd(&s.mass1[(key >> shift) & (bins - 1)], weights.units(x));
                 });
                 __syncthreads();
                 f.key |= (uint32_t)reach(s, s.count1, s.mass1, bins, by_mass, target, f.above, f.mass_above) << shift;
             }
             if (sizeof(T) == 2) f.key = f.key >> 31 ? f.key & 0xffff0000u : f.key | 0xffffu;
             const u64 left = target - (by_mass ? f.mass_above : f.above);  // of the tokens with this value, from 1
-            const u64 w = whole(weight(value_of(f.key)));
+            const u64 w = weights.units(value_of(f.key));
             f.rank = (uint32_t)(by_mass ? (left + w - 1) / w - 1 : left - 1);
             return f;
         };
-        auto mass_to = [&](const Found& f) -> u64 { return f.mass_above + (f.rank + 1) * whole(weight(value_of(f.key))); };
+        auto mass_to = [&](const Found& f) -> u64 { return f.mass_above + (f.rank + 1) * weights.units(value_of(f.key)); };
 
         uint32_t kept = s.total_count;
         kept_mass = s.total_mass;
@@ -214,14 +246,12 @@ __global__ __launch_bounds__(kThreads) void sample_rows(SampleCall call) {
             kept_mass = mass_to(f);
         }
         if (p.top_p < 1.0f) {
-            const double target = ceil((double)fmaxf(p.top_p, 0.0f) * (double)kept_mass);
-            const Found f = find(true, max((u64)1, min((u64)target, kept_mass)));
+            const Found f = find(true, top_p_target(p.top_p, kept_mass));
             kept = min(kept, f.above + f.rank + 1);
             kept_mass = mass_to(f);
         }
         if (min_count < kept) kept_mass = min_mass;
-        const double u = fminf(fmaxf(call.uniforms[r], 0.0f), 1.0f);
-        token = find(true, min((u64)(u * (double)kept_mass) + 1, kept_mass));
+        token = find(true, draw_target(call.uniforms[r], kept_mass));
     }
 
     // Which of the tokens with that value: the rank-th by index.  Counted by chunks of the row, then inside the one it lies in.
@@ -252,13 +282,330 @@ __global__ __launch_bounds__(kThreads) void sample_rows(SampleCall call) {
     if (upto - mine <= rank && rank < upto) {
         uint32_t skip = rank - (upto - mine);
         while (skip-- > 0) bits &= bits - 1;
-        const int index = first + __builtin_ctz(bits);
-        call.tokens[r] = index == call.ids.fork ? APAR_TOKEN_FORK : index == call.ids.child ? APAR_TOKEN_CHILD
-                         : index == call.ids.eos ? APAR_TOKEN_EOS : index;
-        if (call.logprobs) {
-            const double z = greedy || token.key == top ? 0.0 : ((double)value_of(token.key) - x_top) / temperature;
-            call.logprobs[r] = greedy ? 0.0f : (float)(z - log((double)kept_mass / one));
+        write_token(call, r, first + __builtin_ctz(bits));
+        if (call.logprobs) call.logprobs[r] = greedy ? 0.0f : weights.logprob(value_of(token.key), kept_mass);
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void sample_rows(SampleCall call) {
+    __shared__ Shared s;
+    sample_by_digits<T>(s, call, blockIdx.x);
+}
+
+// ---- bf16 rows: a counter per value ---------------------------------------------------------------
+// Inclusive sum over the wavefront's lanes.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t from_lane(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 from_lane(u64 x) {
+    return (u64)from_lane<CTRL, ROWS>((uint32_t)x) | (u64)from_lane<CTRL, ROWS>((uint32_t)(x >> 32)) << 32;
+}
+template <class N>
+__device__ __forceinline__ N prefix_sum(N x) {
+    x += from_lane<0x111, 0xf>(x);  // row_shr 1, 2, 4, 8: within sixteen lanes
+    x += from_lane<0x112, 0xf>(x);
+    x += from_lane<0x114, 0xf>(x);
+    x += from_lane<0x118, 0xf>(x);
+    x += from_lane<0x142, 0xa>(x);  // lane 15 of a row to the next one, lane 31 to the upper half
+    x += from_lane<0x143, 0xc>(x);
+    return x;
+}
+__device__ __forceinline__ uint32_t at_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
+__device__ __forceinline__ u64 at_lane(u64 x, int lane) {
+    return (u64)at_lane((uint32_t)x, lane) | (u64)at_lane((uint32_t)(x >> 32), lane) << 32;
+}
+
+constexpr int kRuns = 1024;  // runs of 64 bit patterns: 0 .. 510 positive values, 512 .. 1021 negative ones, the rest no numbers
+
+struct Counted {
+    uint32_t counts[32768];        // a half word per bit pattern
+    u64 runs_present[128];         // eight bits a run: which of its eighths have a counter that is not 0
+    uint16_t run[kRuns];           // the runs that occur, in order of value
+    uint32_t run_count[kRuns];     // their tokens, then the tokens up to and with them,
+    u64 run_mass[kRuns];           // and masses
+    uint32_t wave_sum[kWaves];
+    uint32_t chunk_count[kSampleMaxVocab / (8 * kThreads) + 3];
+    uint32_t n_runs, tokens;
+    uint32_t pattern, rank;        // the token's value, and which of those with it
+    float logprob;
+};
+union Rooms {
+    Shared digits;
+    Counted counted;
+};
+static_assert(sizeof(Rooms) <= 160 * 1024, "LDS of a compute unit");
+
+__device__ __forceinline__ float bf16_value(uint32_t pattern) { return __uint_as_float(pattern << 16); }
+// The bit pattern of place l in a run: values fall from the largest on.
+__device__ __forceinline__ uint32_t pattern_of(int run, int l) { return (uint32_t)(run * 64 + (run < 512 ? 63 - l : l)); }
+
+// NV: 16-byte pieces of a row per thread, kept in registers (0: rows of any size, read again).
+template <int NV>
+__global__ __launch_bounds__(kThreads) void sample_rows_bf16(SampleCall call) {
+    __shared__ Rooms rooms;
+    Counted& s = rooms.counted;
+    const int r = blockIdx.x, vocab = call.vocab;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const uint16_t* row = (const uint16_t*)call.logits + (int64_t)r * call.row_stride;
+    const int head = min(vocab, (int)((16 - ((uintptr_t)row & 15)) & 15) / 2);
+    const int n_body = (vocab - head) / 8, tail = head + n_body * 8;
+    const u32x4* body = reinterpret_cast<const u32x4*>(row + head);
+    u32x4 v[NV > 0 ? NV : 1];
+    if (NV > 0 && n_body > 0) {  // (past the row's end the last piece again, not looked at: no branch around a load)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = __builtin_nontemporal_load(body + min(i * kThreads + (int)threadIdx.x, n_body - 1));
+    }
+    const int edge = (int)threadIdx.x < head ? (int)threadIdx.x : tail + (int)threadIdx.x - 512;  // a head or (threads from 512 on) a tail element
+    const bool has_edge = (int)threadIdx.x < head || ((int)threadIdx.x >= 512 && edge < vocab);
+    uint32_t edge_pattern = 0xffffu;
+    if (has_edge) edge_pattern = row[edge];
+    const apar_sample_row p = call.rows ? call.rows[r] : apar_sample_row{1.0f, 0, 1.0f, 0.0f};
+    const float u = call.uniforms[r];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<u32x4*>(&s.counts[(i * kThreads + threadIdx.x) * 4]) = u32x4{0u, 0u, 0u, 0u};
+    const int chunks = NV > 0 ? NV : (n_body + kThreads - 1) / kThreads;
+    for (int i = threadIdx.x; i < chunks + 2; i += kThreads) s.chunk_count[i] = 0;
+    __syncthreads();
+
+    // ---- how often each value occurs
+    auto count = [&](uint32_t pattern) { atomicAdd(&s.counts[pattern >> 1], 1u << ((pattern & 1u) * 16)); };
+    auto count_piece = [&](const u32x4& x) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) count(x[j] & 0xffffu), count(x[j] >> 16);
+    };
+    if constexpr (NV > 0) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i * kThreads + (int)threadIdx.x < n_body) count_piece(v[i]);
+    } else {
+        for (int at = threadIdx.x; at < n_body; at += kThreads) count_piece(body[at]);
+    }
+    if (has_edge) count(edge_pattern);
+    __syncthreads();
+    // zeros of both signs are one value
+    bool crowded = false;  // (a counter too small)
+    if (threadIdx.x == 0) {
+        const uint32_t z = (s.counts[0] & 0xffffu) + (s.counts[0x4000] & 0xffffu);
+        s.tokens = z >> 16;
+        s.counts[0] = (s.counts[0] & 0xffff0000u) | (z & 0xffffu);
+        s.counts[0x4000] &= 0xffff0000u;
+    }
+    __syncthreads();
+    // ---- runs that occur (a wavefront looks at 64 of them), their order, and whether any counter overflowed
+    uint32_t all = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(&s.counts[((wave * 8 + i) * 64 + lane) * 4]);
+        all += (x[0] & 0xffffu) + (x[0] >> 16) + (x[1] & 0xffffu) + (x[1] >> 16) + (x[2] & 0xffffu) + (x[2] >> 16) + (x[3] & 0xffffu) + (x[3] >> 16);
+        const u64 present = __builtin_amdgcn_ballot_w64((x[0] | x[1] | x[2] | x[3]) != 0);
+        if (lane == 0) s.runs_present[wave * 8 + i] = present;
+    }
+    all = prefix_sum(all);
+    if (lane == 63) s.wave_sum[wave] = all;
+    __syncthreads();
+    all = 0;
+    for (int w = 0; w < kWaves; ++w) all += s.wave_sum[w];
+    crowded = s.tokens != 0 || all != (uint32_t)vocab;
+    __syncthreads();
+    if (crowded) {  // (every counter's sum is one less, at least, per 65536 tokens that a half word lost)
+        sample_by_digits<uint16_t>(rooms.digits, call, r);
+        return;
+    }
+    {
+        const int t = threadIdx.x;
+        const int run = t <= 510 ? 510 - t : t + 1;  // 510 .. 0, then 512 .. 1021
+        bool here = t < 1021 && ((s.runs_present[run >> 3] >> ((run & 7) * 8)) & 0xffu) != 0;
+        if (run == 510) here = here && (s.counts[0x7f80 / 2] & 0xffffu) != 0;  // +inf; the rest of that run are NaN
+        const u64 which = __builtin_amdgcn_ballot_w64(here);
+        if (lane == 0) s.wave_sum[wave] = __builtin_popcountll(which);
+        __syncthreads();
+        uint32_t before = 0, total = 0;
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) before += s.wave_sum[w];
+            total += s.wave_sum[w];
         }
+        if (here) s.run[before + __builtin_popcountll(which & ((1ull << lane) - 1))] = (uint16_t)run;
+        if (t == 0) s.n_runs = total;
+    }
+    __syncthreads();
+    const int n_runs = s.n_runs;
+    if (n_runs == 0) {  // nothing but -inf and NaN
+        if (threadIdx.x == 0) write_none(call, r);
+        return;
+    }
+    auto counter = [&](int run, int l) -> uint32_t {
+        const uint32_t x = pattern_of(run, l);
+        const uint32_t c = (s.counts[x >> 1] >> ((x & 1u) * 16)) & 0xffffu;
+        return run == 510 && l < 63 ? 0u : c;
+    };
+    const int top_run = __builtin_amdgcn_readfirstlane((int)s.run[0]);
+    const int top_place = __builtin_ctzll(__builtin_amdgcn_ballot_w64(counter(top_run, lane) != 0));
+    const uint32_t top_pattern = pattern_of(top_run, top_place);
+    const bool greedy = !(p.temperature > 0.0f);
+    uint32_t pattern = top_pattern, rank = 0;
+    if (!greedy) {
+        const Weights weights{bf16_value(top_pattern), p.temperature, unit_of(call)};
+        // ---- tokens and mass of every run
+        for (int e = wave; e < n_runs; e += kWaves) {
+            const int run = __builtin_amdgcn_readfirstlane((int)s.run[e]);
+            const uint32_t c = counter(run, lane);
+            u64 m = 0;
+            if (c) m = c * weights.units(bf16_value(pattern_of(run, lane)));
+            const uint32_t tokens = prefix_sum(c);
+            m = prefix_sum(m);
+            if (lane == 63) s.run_count[e] = tokens, s.run_mass[e] = m;
+        }
+        __syncthreads();
+        if (wave == 0) {
+            uint32_t tokens = 0;
+            u64 mass = 0;
+            for (int e0 = 0; e0 < n_runs; e0 += 64) {
+                const int e = e0 + lane;
+                uint32_t c = e < n_runs ? s.run_count[e] : 0;
+                u64 m = e < n_runs ? s.run_mass[e] : 0;
+                c = prefix_sum(c) + tokens;
+                m = prefix_sum(m) + mass;
+                if (e < n_runs) s.run_count[e] = c, s.run_mass[e] = m;
+                tokens = at_lane(c, 63);
+                mass = at_lane(m, 63);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            struct Place {
+                uint32_t pattern, above;  // the value a target is reached on, and what lies above it
+                u64 mass_above, unit;     // its weight
+            };
+            // the first run for which `reached(e)` holds (none: the last one), and the place in it for which `reached_place(tokens, mass, weight)` holds
+            auto find = [&](auto reached, auto reached_place) -> Place {
+                int at = n_runs - 1;
+                for (int e0 = 0; e0 < n_runs; e0 += 64) {
+                    const u64 hit = __builtin_amdgcn_ballot_w64(e0 + lane < n_runs && reached(e0 + lane));
+                    if (hit) {
+                        at = e0 + __builtin_ctzll(hit);
+                        break;
+                    }
+                }
+                const int run = __builtin_amdgcn_readfirstlane((int)s.run[at]);
+                const uint32_t c = counter(run, lane);
+                const uint32_t x = pattern_of(run, lane);
+                const double w = c ? weights.of(bf16_value(x)) : 0.0;
+                const u64 unit = c ? weights.whole(w) : 0;
+                const u64 m = c * unit;
+                const uint32_t before = at ? s.run_count[at - 1] : 0;
+                const u64 mass_before = at ? s.run_mass[at - 1] : 0;
+                const uint32_t ci = prefix_sum(c) + before;
+                const u64 mi = prefix_sum(m) + mass_before;
+                const u64 hit = __builtin_amdgcn_ballot_w64(c != 0 && reached_place(ci, mi, w));
+                if (hit == 0) return Place{0, at_lane(ci, 63), at_lane(mi, 63), 0};  // (only min_p asks for what may be in the next run)
+                const int l = __builtin_ctzll(hit);
+                return Place{at_lane(x, l), at_lane(ci - c, l), at_lane(mi - m, l), at_lane(unit, l)};
+            };
+            auto by_count = [&](uint32_t target) {
+                return find([&](int e) { return s.run_count[e] >= target; }, [&](uint32_t c, u64, double) { return c >= target; });
+            };
+            auto by_mass = [&](u64 target) {
+                return find([&](int e) { return s.run_mass[e] >= target; }, [&](uint32_t, u64 m, double) { return m >= target; });
+            };
+            // of the tokens with the value, the one (from 0) on which the mass is reached
+            auto rank_of = [](const Place& f, u64 target) -> uint32_t { return (uint32_t)((target - f.mass_above + f.unit - 1) / f.unit - 1); };
+            uint32_t kept = tokens;
+            u64 kept_mass = mass;
+            if (p.top_k > 0 && (uint32_t)p.top_k < kept) {
+                const Place f = by_count((uint32_t)p.top_k);
+                kept = (uint32_t)p.top_k;
+                kept_mass = f.mass_above + (kept - f.above) * f.unit;
+            }
+            if (p.top_p < 1.0f) {
+                const u64 target = top_p_target(p.top_p, kept_mass);
+                const Place f = by_mass(target);
+                const uint32_t k = rank_of(f, target);
+                kept = min(kept, f.above + k + 1);
+                kept_mass = f.mass_above + (k + 1) * f.unit;
+            }
+            if (p.min_p > 0.0f) {
+                // what lies above the first value that is too light (the last value of a run stands for the run: it need not occur)
+                const double least = fmin((double)p.min_p, 1.0);
+                const Place f = find([&](int e) { return weights.of(bf16_value(pattern_of(s.run[e], 63))) < least; },
+                                     [&](uint32_t, u64, double w) { return w < least; });
+                if (f.above < kept) kept_mass = f.mass_above;
+            }
+            const u64 target = draw_target(u, kept_mass);
+            const Place f = by_mass(target);
+            if (lane == 0) {
+                s.pattern = f.pattern;
+                s.rank = rank_of(f, target);
+                s.logprob = call.logprobs ? weights.logprob(bf16_value(f.pattern), kept_mass) : 0.0f;
+            }
+        }
+        __syncthreads();
+        pattern = s.pattern;
+        rank = s.rank;
+    }
+
+    // ---- which of the tokens with that value: the rank-th by index, by chunks of the row (head, pieces, tail), then in one
+    const uint32_t both = pattern * 0x10001u, ignored = pattern == 0 ? 0x7fff7fffu : 0xffffffffu;
+    auto matches = [&](const u32x4& x) -> uint32_t {  // bit j: element j
+        uint32_t bits = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t y = (x[j] ^ both) & ignored;
+            bits |= ((y & 0xffffu) == 0 ? 1u : 0u) << (2 * j) | (y >> 16 == 0 ? 2u : 0u) << (2 * j);
+        }
+        return bits;
+    };
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    auto any = [&](const u32x4& x) -> bool {
+        u16x2 least = __builtin_bit_cast(u16x2, (x[0] ^ both) & ignored);
+#pragma unroll
+        for (int j = 1; j < 4; ++j) least = __builtin_elementwise_min(least, __builtin_bit_cast(u16x2, (x[j] ^ both) & ignored));
+        return least.x == 0 || least.y == 0;
+    };
+    const bool edge_matches = has_edge && (edge_pattern ^ (pattern & 0xffffu)) == 0 || (has_edge && pattern == 0 && edge_pattern == 0x8000u);
+    if (edge_matches) atomicAdd(&s.chunk_count[edge < head ? 0 : chunks + 1], 1u);
+    auto count_matches = [&](int i, const u32x4& x) {
+        if (any(x)) atomicAdd(&s.chunk_count[i + 1], (uint32_t)__builtin_popcount(matches(x)));
+    };
+    if constexpr (NV > 0) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i * kThreads + (int)threadIdx.x < n_body) count_matches(i, v[i]);
+    } else {
+        for (int i = 0; i < chunks; ++i)
+            if (i * kThreads + (int)threadIdx.x < n_body) count_matches(i, body[i * kThreads + threadIdx.x]);
+    }
+    __syncthreads();
+    int chunk = 0;
+    while (chunk < chunks + 1 && s.chunk_count[chunk] <= rank) rank -= s.chunk_count[chunk++];
+    chunk = __builtin_amdgcn_readfirstlane(chunk);
+    uint32_t bits = 0;
+    int first = edge;
+    if (chunk == 0 || chunk == chunks + 1) {
+        bits = edge_matches && (edge < head) == (chunk == 0) ? 1u : 0u;
+    } else {
+        const int at = (chunk - 1) * kThreads + (int)threadIdx.x;
+        first = head + at * 8;
+        if constexpr (NV > 0) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (i == chunk - 1 && at < n_body) bits = matches(v[i]);
+        } else {
+            if (at < n_body) bits = matches(body[at]);
+        }
+    }
+    const uint32_t mine = __builtin_popcount(bits);
+    uint32_t upto = prefix_sum(mine);
+    if (lane == 63) s.wave_sum[wave] = upto;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) upto += s.wave_sum[w];
+    if (upto - mine <= rank && rank < upto) {
+        uint32_t skip = rank - (upto - mine);
+        while (skip-- > 0) bits &= bits - 1;
+        write_token(call, r, first + __builtin_ctz(bits));
+        if (call.logprobs) call.logprobs[r] = greedy ? 0.0f : s.logprob;
     }
 }
 
@@ -266,8 +613,13 @@ __global__ __launch_bounds__(kThreads) void sample_rows(SampleCall call) {
 
 hipError_t launch_sample_tokens(const SampleCall& call, bool f32, hipStream_t st) {
     if (call.n <= 0) return hipSuccess;
-    if (f32) hipLaunchKernelGGL(sample_rows<float>, dim3((unsigned)call.n), dim3(kThreads), 0, st, call);
-    else hipLaunchKernelGGL(sample_rows<uint16_t>, dim3((unsigned)call.n), dim3(kThreads), 0, st, call);
+#define APAR_SAMPLE(KERNEL) hipLaunchKernelGGL((KERNEL), dim3((unsigned)call.n), dim3(kThreads), 0, st, call)
+    if (f32) APAR_SAMPLE(sample_rows<float>);
+    else if (call.vocab <= 4 * 8 * kThreads) APAR_SAMPLE(sample_rows_bf16<4>);
+    else if (call.vocab <= 8 * 8 * kThreads) APAR_SAMPLE(sample_rows_bf16<8>);
+    else if (call.vocab <= 16 * 8 * kThreads) APAR_SAMPLE(sample_rows_bf16<16>);
+    else APAR_SAMPLE(sample_rows_bf16<0>);
+#undef APAR_SAMPLE
     return hipGetLastError();
 }
 

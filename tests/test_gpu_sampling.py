@@ -232,3 +232,29 @@ def test_refusals_of_the_binding():
         with pytest.raises(ap.AparError) as e:
             ap.apar_sample_tokens(x, u, tok, workspace=t.empty(need - 1, dtype=t.uint8, device="cuda"))
         assert e.value.status == -7
+
+
+def test_a_value_that_occurs_more_often_than_a_half_word_counts():
+    """bf16 rows are counted value by value in 16 bits; rows with more equal values than that draw the same tokens as fp32 rows do."""
+    t = torch()
+    rng = np.random.default_rng(14)
+    vocab = 150000
+    x = values(rng, 10, vocab, "bf16", 1.0)
+    x[0], x[1, :65535], x[2, :65536], x[3, :131072], x[4, :70000], x[4, 70000:] = 2.0, 1.0, 1.0, -0.5, 0.0, -0.0
+    x[5, 1000:67000], x[6, :140000], x[7, 3:65540] = -float("inf"), float("nan"), 0.25
+    x[8, :65536], x[8, 65536:131073] = 1.0, 0.9921875  # neighbours in one word
+    u = rng.random(10)
+    for params in ([(1.0, 0, 1.0, 0.0)] * 10, [(0.7, 65537, 0.9, 0.05)] * 10, [(1.0, 100000, 1.0, 0.0)] * 10, [(0.0, 0, 1.0, 0.0)] * 10):
+        a, b = call(x, u, params), call(x.float(), u, params)
+        assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+        compare(x, u, params)
+
+
+def test_both_ways_of_counting_agree_to_the_bit():
+    """The same values as bf16 and as fp32: tokens and log-probabilities are equal, whatever the sizes."""
+    rng = np.random.default_rng(15)
+    for n, vocab in ((40, 3), (60, 129), (50, 9000), (20, 32768), (20, 32769), (12, 65537), (12, 131072), (8, 131073), (3, 1 << 20)):
+        x = values(rng, n, vocab, "bf16")
+        u, params = rng.random(n), some_params(rng, n)
+        a, b = call(x, u, params), call(x.float(), u, params)
+        assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
