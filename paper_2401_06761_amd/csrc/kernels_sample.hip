@@ -9,8 +9,8 @@
 // Masses are sums of whole numbers, w 2^weight_bits rounded (42 to 62 bits by the size of the vocabulary, w computed in 64): they
 // do not depend on the order of the additions, and all prefixes agree with each other.
 //
-// bf16 rows (sample_rows_bf16): there are 65536 values, and a workgroup has room to count each of them (128 KiB of LDS, two counters to a
-// word).  A weight is then worked out once per value and not once per token (tens of vector instructions in 64 bits): per run
+// bf16 rows (sample_rows_bf16): there are 65536 values, and a workgroup has room to count each of them (128 KiB of LDS, a word for the
+// two values of a magnitude).  A weight is then worked out once per value and not once per token (tens of vector instructions in 64 bits): per run
 // of 64 values that occur at all, by a wavefront each, to a count and a mass; and every target is reached by one wavefront, first among those
 // runs, then among the 64 values of one.  The row stays in registers for the pass that looks for the token's index.  A value
 // that occurs more than 65535 times shows in the counters' sum; such a row goes through the digits.  Both ways give the same token.
@@ -140,14 +140,37 @@ __device__ __forceinline__ void write_none(const SampleCall& call, int r) {
     if (call.logprobs) call.logprobs[r] = -INFINITY;
 }
 
-// A row's weights: w = exp((x - max) / T), and in whole units.
+// 2^t for t <= 0 in 64 bits: the series of exp(y) up to y^12 for the fraction, |y| <= ln 2 / 2, where y^13 / 13! is 1.7e-16.  (Half the
+// instructions of the library's exp, whose range and special values nobody needs here.)
+__device__ __forceinline__ double exp2_below_one(double t) {
+    if (!(t > -1000.0)) return 0.0;
+    const double n = __builtin_rint(t), y = (t - n) * 0.69314718055994530942;
+    double p = 1.0 / 479001600.0;
+    p = __builtin_fma(p, y, 1.0 / 39916800.0);
+    p = __builtin_fma(p, y, 1.0 / 3628800.0);
+    p = __builtin_fma(p, y, 1.0 / 362880.0);
+    p = __builtin_fma(p, y, 1.0 / 40320.0);
+    p = __builtin_fma(p, y, 1.0 / 5040.0);
+    p = __builtin_fma(p, y, 1.0 / 720.0);
+    p = __builtin_fma(p, y, 1.0 / 120.0);
+    p = __builtin_fma(p, y, 1.0 / 24.0);
+    p = __builtin_fma(p, y, 1.0 / 6.0);
+    p = __builtin_fma(p, y, 0.5);
+    p = __builtin_fma(p, y, 1.0);
+    p = __builtin_fma(p, y, 1.0);
+    return __builtin_ldexp(p, (int)n);
+}
+
+// A row's weights: w = exp((x - max) / T), and in whole units.  `scale`: log2(e) / T.
 struct Weights {
-    double top, temperature, one;
-    __device__ __forceinline__ double of(float x) const { return (double)x == top ? 1.0 : exp(((double)x - top) / temperature); }
+    double top, scale, one;
+    __device__ __forceinline__ Weights(float t, float temperature, double unit)
+        : top(t), scale(1.4426950408889634074 / (double)temperature), one(unit) {}
+    __device__ __forceinline__ double of(float x) const { return (double)x == top ? 1.0 : exp2_below_one(((double)x - top) * scale); }
     __device__ __forceinline__ u64 whole(double w) const { return (u64)(w * one + 0.5); }
     __device__ __forceinline__ u64 units(float x) const { return whole(of(x)); }
     __device__ __forceinline__ float logprob(float x, u64 mass) const {
-        const double z = (double)x == top ? 0.0 : ((double)x - top) / temperature;
+        const double z = (double)x == top ? 0.0 : ((double)x - top) * scale * 0.69314718055994530942;
         return (float)(z - log((double)mass / one));
     }
 };
@@ -185,7 +208,7 @@ __device__ void sample_by_digits(Shared& s, const SampleCall& call, int r) {
         if (threadIdx.x == 0) write_none(call, r);
         return;
     }
-    const Weights weights{value_of(top), p.temperature, unit_of(call)};
+    const Weights weights(value_of(top), p.temperature, unit_of(call));
 
     Found token{top, 0, 0, 0};
     u64 kept_mass = 0;
@@ -318,11 +341,12 @@ __device__ __forceinline__ u64 at_lane(u64 x, int lane) {
     return (u64)at_lane((uint32_t)x, lane) | (u64)at_lane((uint32_t)(x >> 32), lane) << 32;
 }
 
-constexpr int kRuns = 1024;  // runs of 64 bit patterns: 0 .. 510 positive values, 512 .. 1021 negative ones, the rest no numbers
+constexpr int kRuns = 1024;  // runs of 64 bit patterns: 0 .. 510 positive values, 512 .. 1021 negative ones, the others no numbers
 
 struct Counted {
-    uint32_t counts[32768];        // a half word per bit pattern
-    u64 runs_present[128];         // eight bits a run: which of its eighths have a counter that is not 0
+    uint32_t counts[32768];        // per magnitude (bit pattern without the sign): positive values in the low half, negative ones in the high
+    u64 present[128];              // bytes; byte 64 w + 16 k + j, bit i: sixteenth j of run 32 w + 4 i + k has a counter that is not 0 ...
+    u64 present_below[128];        // ... and of the same run of negative values
     uint16_t run[kRuns];           // the runs that occur, in order of value
     uint32_t run_count[kRuns];     // their tokens, then the tokens up to and with them,
     u64 run_mass[kRuns];           // and masses
@@ -330,7 +354,7 @@ struct Counted {
     uint32_t chunk_count[kSampleMaxVocab / (8 * kThreads) + 3];
     uint32_t n_runs, tokens;
     uint32_t pattern, rank;        // the token's value, and which of those with it
-    float logprob;
+    u64 kept_mass;
 };
 union Rooms {
     Shared digits;
@@ -353,10 +377,16 @@ __global__ __launch_bounds__(kThreads) void sample_rows_bf16(SampleCall call) {
     const int head = min(vocab, (int)((16 - ((uintptr_t)row & 15)) & 15) / 2);
     const int n_body = (vocab - head) / 8, tail = head + n_body * 8;
     const u32x4* body = reinterpret_cast<const u32x4*>(row + head);
+    // Pieces on their way: a few at a time, others behind those that are counted (all at once, the wavefronts stand at their own loads
+    // for as long as the row takes, and nobody counts).
+    constexpr int kAhead = NV < 4 ? NV : 4;
     u32x4 v[NV > 0 ? NV : 1];
-    if (NV > 0 && n_body > 0) {  // (past the row's end the last piece again, not looked at: no branch around a load)
+    auto fetch = [&](int i) {  // (past the row's end the last piece again, not looked at: no branch around a load)
+        v[i] = __builtin_nontemporal_load(body + min(i * kThreads + (int)threadIdx.x, n_body - 1));
+    };
+    if (NV > 0 && n_body > 0) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) v[i] = __builtin_nontemporal_load(body + min(i * kThreads + (int)threadIdx.x, n_body - 1));
+        for (int i = 0; i < kAhead; ++i) fetch(i);
     }
     const int edge = (int)threadIdx.x < head ? (int)threadIdx.x : tail + (int)threadIdx.x - 512;  // a head or (threads from 512 on) a tail element
     const bool has_edge = (int)threadIdx.x < head || ((int)threadIdx.x >= 512 && edge < vocab);
@@ -368,18 +398,28 @@ __global__ __launch_bounds__(kThreads) void sample_rows_bf16(SampleCall call) {
     for (int i = 0; i < 8; ++i) *reinterpret_cast<u32x4*>(&s.counts[(i * kThreads + threadIdx.x) * 4]) = u32x4{0u, 0u, 0u, 0u};
     const int chunks = NV > 0 ? NV : (n_body + kThreads - 1) / kThreads;
     for (int i = threadIdx.x; i < chunks + 2; i += kThreads) s.chunk_count[i] = 0;
-    __syncthreads();
+    // (a barrier for LDS alone: the row is still on its way, and its first pieces are counted while the others come)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
 
     // ---- how often each value occurs
-    auto count = [&](uint32_t pattern) { atomicAdd(&s.counts[pattern >> 1], 1u << ((pattern & 1u) * 16)); };
+    auto count = [&](uint32_t pattern) { atomicAdd(&s.counts[pattern & 0x7fffu], 1u + (pattern >> 15) * 0xffffu); };
     auto count_piece = [&](const u32x4& x) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) count(x[j] & 0xffffu), count(x[j] >> 16);
     };
     if constexpr (NV > 0) {
+        if (n_body > 0) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (i * kThreads + (int)threadIdx.x < n_body) count_piece(v[i]);
+            for (int i = 0; i < NV; ++i) {
+                if (i + kAhead < NV) fetch(i + kAhead);
+                asm volatile("" ::: "memory");
+                if (i * kThreads + (int)threadIdx.x < n_body) count_piece(v[i]);
+                asm volatile("" ::: "memory");
+            }
+        }
     } else {
         for (int at = threadIdx.x; at < n_body; at += kThreads) count_piece(body[at]);
     }
@@ -388,27 +428,32 @@ __global__ __launch_bounds__(kThreads) void sample_rows_bf16(SampleCall call) {
     // zeros of both signs are one value
     bool crowded = false;  // (a counter too small)
     if (threadIdx.x == 0) {
-        const uint32_t z = (s.counts[0] & 0xffffu) + (s.counts[0x4000] & 0xffffu);
+        const uint32_t z = (s.counts[0] & 0xffffu) + (s.counts[0] >> 16);
         s.tokens = z >> 16;
-        s.counts[0] = (s.counts[0] & 0xffff0000u) | (z & 0xffffu);
-        s.counts[0x4000] &= 0xffff0000u;
+        s.counts[0] = z & 0xffffu;
     }
     __syncthreads();
-    // ---- runs that occur (a wavefront looks at 64 of them), their order, and whether any counter overflowed
-    uint32_t all = 0;
+    // ---- runs that occur (a wavefront looks at 32 of either sign), their order, and whether any counter overflowed
+    uint32_t all = 0, up = 0, down = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 8; ++i) {  // (a run is sixteen lanes' pieces)
         const u32x4 x = *reinterpret_cast<const u32x4*>(&s.counts[((wave * 8 + i) * 64 + lane) * 4]);
-        all += (x[0] & 0xffffu) + (x[0] >> 16) + (x[1] & 0xffffu) + (x[1] >> 16) + (x[2] & 0xffffu) + (x[2] >> 16) + (x[3] & 0xffffu) + (x[3] >> 16);
-        const u64 present = __builtin_amdgcn_ballot_w64((x[0] | x[1] | x[2] | x[3]) != 0);
-        if (lane == 0) s.runs_present[wave * 8 + i] = present;
+        const uint32_t any = x[0] | x[1] | x[2] | x[3];
+        up |= (any & 0xffffu) != 0 ? 1u << i : 0u;
+        down |= any >> 16 != 0 ? 1u << i : 0u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) all = __builtin_amdgcn_sad_u16(x[j], 0u, all);  // (both half words)
     }
-    all = prefix_sum(all);
-    if (lane == 63) s.wave_sum[wave] = all;
-    __syncthreads();
-    all = 0;
-    for (int w = 0; w < kWaves; ++w) all += s.wave_sum[w];
-    crowded = s.tokens != 0 || all != (uint32_t)vocab;
+    reinterpret_cast<uint8_t*>(s.present)[wave * 64 + lane] = (uint8_t)up;
+    reinterpret_cast<uint8_t*>(s.present_below)[wave * 64 + lane] = (uint8_t)down;
+    if (vocab > 65535) {
+        all = prefix_sum(all);
+        if (lane == 63) s.wave_sum[wave] = all;
+        __syncthreads();
+        all = 0;
+        for (int w = 0; w < kWaves; ++w) all += s.wave_sum[w];
+        crowded = s.tokens != 0 || all != (uint32_t)vocab;
+    }
     __syncthreads();
     if (crowded) {  // (every counter's sum is one less, at least, per 65536 tokens that a half word lost)
         sample_by_digits<uint16_t>(rooms.digits, call, r);
@@ -417,8 +462,10 @@ __global__ __launch_bounds__(kThreads) void sample_rows_bf16(SampleCall call) {
     {
         const int t = threadIdx.x;
         const int run = t <= 510 ? 510 - t : t + 1;  // 510 .. 0, then 512 .. 1021
-        bool here = t < 1021 && ((s.runs_present[run >> 3] >> ((run & 7) * 8)) & 0xffu) != 0;
-        if (run == 510) here = here && (s.counts[0x7f80 / 2] & 0xffffu) != 0;  // +inf; the rest of that run are NaN
+        const u64* flags = run < 512 ? s.present : s.present_below;
+        const int at = ((run & 511) >> 5) * 8 + (run & 3) * 2;
+        bool here = t < 1021 && (((flags[at] | flags[at + 1]) >> ((run >> 2) & 7)) & 0x0101010101010101ull) != 0;
+        if (run == 510) here = here && (s.counts[0x7f80] & 0xffffu) != 0;  // +inf; the rest of that run are NaN
         const u64 which = __builtin_amdgcn_ballot_w64(here);
         if (lane == 0) s.wave_sum[wave] = __builtin_popcountll(which);
         __syncthreads();
@@ -437,9 +484,8 @@ __global__ __launch_bounds__(kThreads) void sample_rows_bf16(SampleCall call) {
         return;
     }
     auto counter = [&](int run, int l) -> uint32_t {
-        const uint32_t x = pattern_of(run, l);
-        const uint32_t c = (s.counts[x >> 1] >> ((x & 1u) * 16)) & 0xffffu;
-        return run == 510 && l < 63 ? 0u : c;
+        const uint32_t x = pattern_of(run, l), c = s.counts[x & 0x7fffu];
+        return run == 510 && l < 63 ? 0u : run < 512 ? c & 0xffffu : c >> 16;
     };
     const int top_run = __builtin_amdgcn_readfirstlane((int)s.run[0]);
     const int top_place = __builtin_ctzll(__builtin_amdgcn_ballot_w64(counter(top_run, lane) != 0));
@@ -447,7 +493,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_bf16(SampleCall call) {
     const bool greedy = !(p.temperature > 0.0f);
     uint32_t pattern = top_pattern, rank = 0;
     if (!greedy) {
-        const Weights weights{bf16_value(top_pattern), p.temperature, unit_of(call)};
+        const Weights weights(bf16_value(top_pattern), p.temperature, unit_of(call));
         // ---- tokens and mass of every run
         for (int e = wave; e < n_runs; e += kWaves) {
             const int run = __builtin_amdgcn_readfirstlane((int)s.run[e]);
@@ -535,19 +581,18 @@ __global__ __launch_bounds__(kThreads) void sample_rows_bf16(SampleCall call) {
             }
             const u64 target = draw_target(u, kept_mass);
             const Place f = by_mass(target);
-            if (lane == 0) {
-                s.pattern = f.pattern;
-                s.rank = rank_of(f, target);
-                s.logprob = call.logprobs ? weights.logprob(bf16_value(f.pattern), kept_mass) : 0.0f;
-            }
+            if (lane == 0) s.pattern = f.pattern, s.rank = rank_of(f, target), s.kept_mass = kept_mass;
         }
         __syncthreads();
         pattern = s.pattern;
         rank = s.rank;
+        if (call.logprobs && threadIdx.x == kThreads - 1) call.logprobs[r] = weights.logprob(bf16_value(pattern), s.kept_mass);
+    } else if (call.logprobs && threadIdx.x == 0) {
+        call.logprobs[r] = 0.0f;
     }
 
     // ---- which of the tokens with that value: the rank-th by index, by chunks of the row (head, pieces, tail), then in one
-    const uint32_t both = pattern * 0x10001u, ignored = pattern == 0 ? 0x7fff7fffu : 0xffffffffu;
+    const uint32_t both = pattern * 0x10001u, ignored = pattern == 0 ? 0x7fff7fffu : 0xffffffffu;  // (zeros: of either sign)
     auto matches = [&](const u32x4& x) -> uint32_t {  // bit j: element j
         uint32_t bits = 0;
 #pragma unroll
@@ -558,11 +603,12 @@ __global__ __launch_bounds__(kThreads) void sample_rows_bf16(SampleCall call) {
         return bits;
     };
     typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-    auto any = [&](const u32x4& x) -> bool {
-        u16x2 least = __builtin_bit_cast(u16x2, (x[0] ^ both) & ignored);
+    auto any = [&](const u32x4& x) -> bool {  // (for zeros: perhaps)
+        u16x2 least = {0xffff, 0xffff};
 #pragma unroll
-        for (int j = 1; j < 4; ++j) least = __builtin_elementwise_min(least, __builtin_bit_cast(u16x2, (x[j] ^ both) & ignored));
-        return least.x == 0 || least.y == 0;
+        for (int j = 0; j < 4; ++j) least = __builtin_elementwise_min(least, __builtin_bit_cast(u16x2, x[j] ^ both));
+        const uint32_t l = __builtin_bit_cast(uint32_t, least);
+        return (l & 0xffffu) == 0 || l >> 16 == 0 || pattern == 0;
     };
     const bool edge_matches = has_edge && (edge_pattern ^ (pattern & 0xffffu)) == 0 || (has_edge && pattern == 0 && edge_pattern == 0x8000u);
     if (edge_matches) atomicAdd(&s.chunk_count[edge < head ? 0 : chunks + 1], 1u);
@@ -605,7 +651,6 @@ __global__ __launch_bounds__(kThreads) void sample_rows_bf16(SampleCall call) {
         uint32_t skip = rank - (upto - mine);
         while (skip-- > 0) bits &= bits - 1;
         write_token(call, r, first + __builtin_ctz(bits));
-        if (call.logprobs) call.logprobs[r] = greedy ? 0.0f : s.logprob;
     }
 }
 
