@@ -11,7 +11,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libapar.so")
 SOURCES = ["apar_pool.cpp", "plan.cpp", "controller.cpp", "kernels_misc.hip", "kernels_attn_bf16.hip", "kernels_few_bf16.hip", "kernels_attn_f32.hip", "kernels_matrix_bf16.hip",
-           "kernels_attn_fp4.hip", "kernels_append_fp4.hip", "rotary.cpp", "kernels_rotary.hip", "sample.cpp", "kernels_sample.hip"]
+           "kernels_attn_fp4.hip", "kernels_matrix_fp4.hip", "kernels_append_fp4.hip", "rotary.cpp", "kernels_rotary.hip", "sample.cpp", "kernels_sample.hip"]
 
 
 def hipcc() -> str:

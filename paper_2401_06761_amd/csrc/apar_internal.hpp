@@ -335,6 +335,8 @@ hipError_t launch_append_fp4(const Shape& s, void* pool, const void* k, const vo
                              int n_blocks, int n_open, int n_src, hipStream_t st);
 hipError_t launch_read_rows_fp4(const Shape& s, const void* pool, const int32_t* src_codes, int n_rows, void* k_out, void* v_out,
                                 hipStream_t st);
+hipError_t launch_prefill_fp4(const Shape& s, const void* pool, const void* q, const PrefillWg* wgs, const int32_t* tables, int n_wg,
+                              void* out, hipStream_t st);
 hipError_t launch_prefill_bf16(const Shape& s, const void* pool, const void* q, const PrefillWg* wgs,
                                const int32_t* tables, int n_wg, void* out, hipStream_t st);
 // workgroups [wg_first, wg_first + n_wg) of the plan: matrix units (row_tiles byte = kMatrixUnitRows)

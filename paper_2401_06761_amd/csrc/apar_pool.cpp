@@ -884,10 +884,17 @@ int decode_common(apar_pool* p, const void* q, const void* cand_k, const void* c
 //    440 / 437, group 1, 891 threads, walks around 700 1224 / 1172; and calls whose query tokens attend to kMatrixPrefillMeanWalk rows
 //    on average go there (group 1, one token each, 362 threads, around 1100 rows: 499 / 523 where six share a prefix, 1080 / 1077 where
 //    nobody does).  fp8 pools: neither (362 threads, group 4, around 1050 rows, 32 and 64 rows 170 / 156, 170 / 184).
+//  - 4-bit pools: a tile is widened once per workgroup there, and once per 16 or 32 rows on the row tiles (row tiles / matrix kernel; 362 threads,
+//    six to a shared prefix, walks of 400): group 1, 2, 4, 16, 64, 128 rows 355 / 261, 423 / 263, 433 / 266, 427 / 319, 582 / 422; group 4, 8,
+//    16, 64, 128 rows 112 / 83, 121 / 81, 139 / 102, 187 / 116; group 8, 8 and 16 rows 41 / 30, 43 / 29; group 16, 16 rows 61 / 37; walks of 1050
+//    alike; 5 prompts of 4000, group 4 1034 / 684, one of 40 16 / 15.  Only where most threads have one token of few heads do rows of
+//    several threads share tiles: group 1 176 / 267, group 4 61 / 81, walks of 1050 438 / 540, 130 / 161; with 8 threads 23 / 19, 24 / 20,
+//    with 40 of 3000, which share nothing, 195 / 186, 97 / 76.
 constexpr int64_t kMatrixPrefillRows = 64, kMatrixPrefillMinRows = 32;
 constexpr int64_t kMatrixPrefillWalked = 4500000;
 constexpr int64_t kMatrixPrefillMeanWalk = 1024;
 bool prefill_on_matrix(const Shape& s, const std::vector<PrefillThreadView>& views, int64_t rows, int64_t attended) {
+    if (s.fp4) return rows >= 2 * (int64_t)views.size() || s.group > 4 || (int64_t)views.size() * s.n_kv < 2048;
     const int64_t chunk = 128 / s.group;
     int64_t wgs = 0, wide = 0, narrow = 0;
     for (const PrefillThreadView& t : views) {
@@ -896,7 +903,7 @@ bool prefill_on_matrix(const Shape& s, const std::vector<PrefillThreadView>& vie
         ((int64_t)t.m * s.group > kMatrixPrefillRows ? wide : narrow) += w * (t.len - t.m) + chunk * (w - 1) * w / 2 + t.m;
     }
     if (wide >= narrow) return true;
-    if (s.fp8_sealed || s.fp4) return false;
+    if (s.fp8_sealed) return false;
     return attended >= kMatrixPrefillMeanWalk * rows ||
            (rows * s.group >= kMatrixPrefillMinRows * wgs && (wide + narrow) * s.n_kv >= kMatrixPrefillWalked);
 }
@@ -1010,7 +1017,7 @@ int prefill_common(apar_pool* p, const void* q, const apar_thread* ids, const in
     int rc = APAR_OK;
     p->last_prefill_kernel = APAR_PREFILL_ROW_TILES;
     // (an fp8 pool takes the matrix kernel by AUTO only)
-    if (!p->dry_run && p->shape.dtype == APAR_BF16 && !p->shape.fp4 && 16 % p->shape.group == 0 &&
+    if (!p->dry_run && p->shape.dtype == APAR_BF16 && 16 % p->shape.group == 0 &&
         ((p->prefill_kernel == APAR_PREFILL_MATRIX && !p->shape.fp8_sealed) ||
          (p->prefill_kernel == APAR_PREFILL_AUTO && prefill_on_matrix(p->shape, views, rows, attended)))) {
         p->last_prefill_kernel = APAR_PREFILL_MATRIX;

@@ -30,6 +30,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstring>
+#include <type_traits>
 
 #include "apar_internal.hpp"
 #include "attn_split.hpp"
@@ -184,12 +185,24 @@ __device__ __forceinline__ void accumulate(const uint32_t (&wa)[4][4], const uin
     }
 }
 
-constexpr int kFoldFloats = 8 * 256 + 32;  // one wavefront's states: eight accumulator quads per lane, reference and sum per row
+constexpr int kFoldFloats = 8 * 256 + 128;  // one wavefront's state: eight accumulator quads, reference and share of the sum per lane
+
+template <bool SPLIT, bool INLINE>
+__device__ __forceinline__ Slice unit_of_block(PlanDev& plan, int n_kv) {
+    if constexpr (INLINE) plan_from_arguments(plan);
+    Slice slice;
+    if constexpr (SPLIT) {
+        slice = slice_of_block(plan.split, 0, n_kv);
+    } else {
+        slice.wg = blockIdx.x / n_kv;
+    }
+    return slice;
+}
 
 // NT = 16-row tiles per wavefront; SPLIT: several workgroups per unit, each with a slice of its lists (attn_split.hpp).
-// lds: three wavefronts' row states when a unit is split
+// lds: the wavefronts' row states when a unit is divided among them
 template <int NT, bool SPLIT>
-__device__ __forceinline__ void attend_unit(float (&lds)[3][kFoldFloats], const Slice& slice, const char* __restrict__ pool,
+__device__ __forceinline__ void attend_unit(float (&lds)[4][kFoldFloats], const Slice& slice, const char* __restrict__ pool,
                                             const uint16_t* __restrict__ q, const PlanDev& plan, int n_cand, int n_q, int n_kv, int group,
                                             float scale_log2e, const PartialBuf& part, const uint16_t* __restrict__ cand_k,
                                             const uint16_t* __restrict__ cand_v, const uint8_t* __restrict__ cand_mask,
@@ -244,66 +257,84 @@ __device__ __forceinline__ void attend_unit(float (&lds)[3][kFoldFloats], const 
         const int fill = (meta >> 20) & 31;
         return (meta >> 30) ? min(fill, max(0, ((meta >> 25) & 31) + ahead)) : fill;
     };
+    const uint32_t k_ofs = c * 64 + g4 * 16, v_ofs = kFp4V + lane * 16;
+    const uint32_t ks_ofs = kFp4KScale + c * 4 + g4, vs_ofs = kFp4VScale + g4 * 16 + (c & 12);
     auto fetch = [&](int blk) -> Raw {
         const char* tile = head_base + blk * block_stride;
         Raw t;
-        t.k = *reinterpret_cast<const u32x4*>(tile + c * 64 + g4 * 16);
-        t.v = *reinterpret_cast<const u32x4*>(tile + kFp4V + lane * 16);
-        t.ks = *reinterpret_cast<const uint8_t*>(tile + kFp4KScale + c * 4 + g4);
-        t.vs = *reinterpret_cast<const uint32_t*>(tile + kFp4VScale + g4 * 16 + (c & 12));
+        t.k = *reinterpret_cast<const u32x4*>(tile + k_ofs);
+        t.v = *reinterpret_cast<const u32x4*>(tile + v_ofs);
+        t.ks = *reinterpret_cast<const uint8_t*>(tile + ks_ofs);
+        t.vs = *reinterpret_cast<const uint32_t*>(tile + vs_ofs);
         return t;
     };
-    // both lists, one after the other; `shift`: the shared list's ranges count row groups from the workgroup's first
+    // Both lists, one after the other; `shift`: the shared list's ranges count row groups from the workgroup's first.  The words of the
+    // pair after the next one are on their way while the next one's tiles are.
     for (int list = 0; list < 2; ++list) {
         const TileRef* tiles = plan.tiles + (list == 0 ? coop_ofs : wi.tile_ofs);
         const int n = list == 0 ? n_coop : wi.n_tiles;
         const int shift = list == 0 ? wi.grp_lo - wg->grp_base : 0;
-        // (tiles of the shared list that no row of this wavefront sees are passed over)
+        if (n == 0) continue;
+        // Tiles of the shared list that no row of this wavefront sees are passed over; its own list has none.
         auto next = [&](int t) {
-            for (; t < n; ++t) {
+            for (; list == 0 && t < n; ++t) {
                 const int meta = tiles[t].meta;
                 if ((meta & 1023) - shift < wi.n_grp && ((meta >> 10) & 1023) - shift > 0) break;
             }
             return t;
         };
-        // the pair that starts at or behind t; without a second tile the first one again, seen by nobody
-        auto pair_at = [&](int t, TileRef& a, TileRef& b) -> int {
-            t = next(t);
-            a = tiles[min(t, n - 1)];  // (past the end: the last tile once more, not used)
-            const int u = next(t + 1);
-            b = u < n ? tiles[u] : TileRef{a.blk, 0};
-            return t < n ? u + 1 : n + 2;
+        struct Pair {
+            TileRef a, b;
+            bool any;
         };
-        if (n == 0) continue;
-        TileRef a, b;
-        int t = pair_at(0, a, b);
-        if (t > n + 1) continue;
-        Raw ta = fetch(a.blk), tb = fetch(b.blk);
+        int t = 0;
+        // the pair from t on; without a second tile the first one again, seen by nobody; past the end the last tile, not used
+        auto next_pair = [&]() -> Pair {
+            Pair p;
+            t = next(t);
+            p.any = t < n;
+            p.a = tiles[min(t, n - 1)];
+            t = next(t + 1);
+            p.b = tiles[min(t, n - 1)];
+            if (t >= n) p.b = TileRef{p.a.blk, 0};
+            ++t;
+            return p;
+        };
+        // does every row group of the wavefront see all of the tile?
+        auto whole = [&](int meta) {
+            return (meta & 1023) - shift <= 0 && ((meta >> 10) & 1023) - shift >= wi.n_grp && meta >> 20 == 16;
+        };
+        Pair p = next_pair();
+        if (!p.any) continue;
+        Raw ta = fetch(p.a.blk), tb = fetch(p.b.blk);
+        Pair p1 = next_pair();
         while (true) {
-            TileRef na, nb;
-            const int tn = pair_at(t, na, nb);
-            const Raw xa = fetch(na.blk), xb = fetch(nb.blk);
+            const Raw xa = fetch(p1.a.blk), xb = fetch(p1.b.blk);
+            const Pair p2 = next_pair();
             f32x4 sa[NT], sb[NT];
             uint32_t wa[4][4], wb[4][4];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) sa[nt] = products(ta, st[nt]), sb[nt] = products(tb, st[nt]);
             widen(ta, wa);
             widen(tb, wb);
-            const int alo = (a.meta & 1023) - shift, ahi = ((a.meta >> 10) & 1023) - shift;
-            const int blo = (b.meta & 1023) - shift, bhi = ((b.meta >> 10) & 1023) - shift;
+            if (!(whole(p.a.meta) && whole(p.b.meta))) {  // (rows that are none take part in whole tiles: nobody writes them)
+                const int alo = (p.a.meta & 1023) - shift, ahi = ((p.a.meta >> 10) & 1023) - shift;
+                const int blo = (p.b.meta & 1023) - shift, bhi = ((p.b.meta >> 10) & 1023) - shift;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const int mine_a = (my_j[nt] >= max(alo, 0) && my_j[nt] < ahi ? seen(a.meta, my_j[nt] - alo) : 0) - 4 * g4;
-                const int mine_b = (my_j[nt] >= max(blo, 0) && my_j[nt] < bhi ? seen(b.meta, my_j[nt] - blo) : 0) - 4 * g4;
+                for (int nt = 0; nt < NT; ++nt) {
+                    const int mine_a = (my_j[nt] >= max(alo, 0) && my_j[nt] < ahi ? seen(p.a.meta, my_j[nt] - alo) : 0) - 4 * g4;
+                    const int mine_b = (my_j[nt] >= max(blo, 0) && my_j[nt] < bhi ? seen(p.b.meta, my_j[nt] - blo) : 0) - 4 * g4;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    sa[nt][i] = i < mine_a ? sa[nt][i] : -INFINITY;
-                    sb[nt][i] = i < mine_b ? sb[nt][i] : -INFINITY;
+                    for (int i = 0; i < 4; ++i) {
+                        sa[nt][i] = i < mine_a ? sa[nt][i] : -INFINITY;
+                        sb[nt][i] = i < mine_b ? sb[nt][i] : -INFINITY;
+                    }
                 }
-                accumulate(wa, wb, st[nt], sa[nt], sb[nt], scale_log2e);
             }
-            if (tn > n + 1) break;
-            a = na, b = nb, ta = xa, tb = xb, t = tn;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) accumulate(wa, wb, st[nt], sa[nt], sb[nt], scale_log2e);
+            if (!p1.any) break;
+            p = p1, p1 = p2, ta = xa, tb = xb;
         }
     }
 
@@ -376,71 +407,96 @@ __device__ __forceinline__ void attend_unit(float (&lds)[3][kFoldFloats], const 
     }
 
     // ---- results --------------------------------------------------------------------------------
-    if (NT == 1 && (wi.flags & kWaveSplit)) {
-        // the four wavefronts hold the same rows over different tiles: fold 1..3 into 0 through LDS
-        Row& s0 = st[0];
-        float lt = s0.l;
-        lt += __shfl_xor(lt, 16, 64);
-        lt += __shfl_xor(lt, 32, 64);
-        if (wave > 0) {
-            float* to = lds[wave - 1];
-#pragma unroll
-            for (int jj = 0; jj < 8; ++jj) *reinterpret_cast<f32x4*>(to + (jj * 64 + lane) * 4) = s0.o[jj];
-            if (g4 == 0) to[2048 + 2 * c] = s0.m, to[2048 + 2 * c + 1] = lt;
-        }
-        __syncthreads();
-        if (wave > 0) return;
-        float mx = s0.m;
-        for (int w2 = 0; w2 < 3; ++w2) mx = fmaxf(mx, lds[w2][2048 + 2 * c]);
-        // a wavefront that saw no tile of a row left m = -inf and sums of zero for it
-        const float a0 = (s0.m == -INFINITY) ? 1.0f : __builtin_amdgcn_exp2f(s0.m - mx);
-        lt *= a0;
-#pragma unroll
-        for (int jj = 0; jj < 8; ++jj) s0.o[jj] *= a0;
-        for (int w2 = 0; w2 < 3; ++w2) {
-            const float mw = lds[w2][2048 + 2 * c];
-            if (mw == -INFINITY && lds[w2][2048 + 2 * c + 1] == 0.0f) continue;
-            const float aw = __builtin_amdgcn_exp2f(mw - mx);
-            lt += aw * lds[w2][2048 + 2 * c + 1];
-#pragma unroll
-            for (int jj = 0; jj < 8; ++jj) s0.o[jj] += aw * *reinterpret_cast<const f32x4*>(&lds[w2][(jj * 64 + lane) * 4]);
-        }
-        s0.m = mx;
-        s0.l = g4 == 0 ? lt : 0.0f;
-    }
-    if constexpr (SPLIT)
-        if (!fold_slices<NT, 8>(plan.split, slice, n_kv, kvh, wave, (wi.flags & kWaveSplit) ? 1 : 4, lane, st)) return;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
+    // Accumulators j0 .. j0 + J - 1 of the lane's row of row tile nt: the dims 8 (4 g + i) + jj.
+    auto write = [&](auto count, int j0, int nt) {
+        constexpr int J = decltype(count)::value;
         float lt = st[nt].l;
         lt += __shfl_xor(lt, 16, 64);
         lt += __shfl_xor(lt, 32, 64);
         int j, listed, cc;
         int64_t qrow, slot;
-        if (!row_of(nt, c, j, listed, cc, qrow, slot)) continue;
+        if (!row_of(nt, c, j, listed, cc, qrow, slot)) return;
         if (wi.flags & kWaveDirect) {
             const float inv = 1.0f / lt;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                u32x4 x;
+                uint32_t x[J / 2];
 #pragma unroll
-                for (int h = 0; h < 4; ++h) x[h] = pack_pair(st[nt].o[2 * h][i] * inv, st[nt].o[2 * h + 1][i] * inv);
-                *reinterpret_cast<u32x4*>(out + qrow * 128 + 32 * g4 + 8 * i) = x;
+                for (int h = 0; h < J / 2; ++h) x[h] = pack_pair(st[nt].o[2 * h][i] * inv, st[nt].o[2 * h + 1][i] * inv);
+                uint16_t* to = out + qrow * 128 + 32 * g4 + 8 * i + j0;
+                if constexpr (J == 8) *reinterpret_cast<u32x4*>(to) = u32x4{x[0], x[1], x[2], x[3]};
+                else *reinterpret_cast<uint32_t*>(to) = x[0];
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i) {
+                float* to = part.o + slot * 128 + 32 * g4 + 8 * i + j0;
+                if constexpr (J == 8) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const f32x4 x = {st[nt].o[4 * h][i], st[nt].o[4 * h + 1][i], st[nt].o[4 * h + 2][i], st[nt].o[4 * h + 3][i]};
-                    *reinterpret_cast<f32x4*>(part.o + slot * 128 + 32 * g4 + 8 * i + 4 * h) = x;
+                    for (int h = 0; h < 2; ++h)
+                        *reinterpret_cast<f32x4*>(to + 4 * h) =
+                            f32x4{st[nt].o[4 * h][i], st[nt].o[4 * h + 1][i], st[nt].o[4 * h + 2][i], st[nt].o[4 * h + 3][i]};
+                } else {
+                    *reinterpret_cast<f32x2*>(to) = f32x2{st[nt].o[0][i], st[nt].o[1][i]};
                 }
-            if (g4 == 0) {
+            }
+            if (g4 == 0 && j0 == 0) {
                 part.ml[slot * 2] = st[nt].m;
                 part.ml[slot * 2 + 1] = lt;
             }
         }
+    };
+    if (NT == 1 && (wi.flags & kWaveSplit)) {
+        // the four wavefronts hold the same rows over different tiles: every one folds two of the eight accumulators, of its
+        // workgroup's wavefronts through LDS and then of the unit's slices.  (One wavefront folding all of the slices: one thread family of 32 k
+        // tokens, 8 kv heads, 32 slices 27.6 us a call, this way FOLD_US.)
+        float* to = lds[wave];
+#pragma unroll
+        for (int jj = 0; jj < 8; ++jj) *reinterpret_cast<f32x4*>(to + (jj * 64 + lane) * 4) = st[0].o[jj];
+        *reinterpret_cast<f32x2*>(to + 2048 + lane * 2) = f32x2{st[0].m, st[0].l};
+        __syncthreads();
+        const int j0 = 2 * wave;
+        f32x2 ml[4];
+        f32x4 o[4][2];
+#pragma unroll
+        for (int w2 = 0; w2 < 4; ++w2) {
+            ml[w2] = *reinterpret_cast<const f32x2*>(&lds[w2][2048 + lane * 2]);
+#pragma unroll
+            for (int jj = 0; jj < 2; ++jj) o[w2][jj] = *reinterpret_cast<const f32x4*>(&lds[w2][((j0 + jj) * 64 + lane) * 4]);
+        }
+        const float mx = fmaxf(fmaxf(ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0]));
+        st[0].m = mx;
+        st[0].l = 0.0f;
+        st[0].o[0] = st[0].o[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w2 = 0; w2 < 4; ++w2) {
+            // a wavefront that saw no tile of a row left m = -inf and sums of zero for it
+            const float a = ml[w2][0] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml[w2][0] - mx);
+            st[0].l += a * ml[w2][1];
+            st[0].o[0] += a * o[w2][0];
+            st[0].o[1] += a * o[w2][1];
+        }
+        if constexpr (SPLIT)
+            if (!fold_slices<1, 2, 8>(plan.split, slice, n_kv, kvh, wave, 1, lane, reinterpret_cast<Row(&)[1]>(st), j0)) return;
+        write(std::integral_constant<int, 2>{}, j0, 0);
+        return;
     }
+    if constexpr (SPLIT)
+        if (!fold_slices<NT, 8>(plan.split, slice, n_kv, kvh, wave, 4, lane, st)) return;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) write(std::integral_constant<int, 8>{}, 0, nt);
+}
+
+// Units of one row tile per wavefront.
+template <bool SPLIT, bool INLINE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void attention_fp4_one(
+    PlanWords<INLINE>, const char* __restrict__ pool, const uint16_t* __restrict__ q, PlanDev plan, int n_cand, int n_q, int n_kv, int group,
+    float scale_log2e, PartialBuf part, const uint16_t* __restrict__ cand_k, const uint16_t* __restrict__ cand_v,
+    const uint8_t* __restrict__ cand_mask, uint16_t* __restrict__ out) {
+    __shared__ __attribute__((aligned(16))) float lds[4][kFoldFloats];
+    const Slice slice = unit_of_block<SPLIT, INLINE>(plan, n_kv);
+    tables_unwritten(plan);
+    attend_unit<1, SPLIT>(lds, slice, pool, q, plan, n_cand, n_q, n_kv, group, scale_log2e, part, cand_k, cand_v, cand_mask, out);
 }
 
 // Units of either row-tile class, in one launch.  INLINE (with SPLIT): the plan's tables come with the kernel's arguments.
@@ -449,14 +505,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
     PlanWords<INLINE>, const char* __restrict__ pool, const uint16_t* __restrict__ q, PlanDev plan, int n_cand, int n_q, int n_kv, int group,
     float scale_log2e, PartialBuf part, const uint16_t* __restrict__ cand_k, const uint16_t* __restrict__ cand_v,
     const uint8_t* __restrict__ cand_mask, uint16_t* __restrict__ out) {
-    __shared__ __attribute__((aligned(16))) float lds[3][kFoldFloats];
-    if constexpr (INLINE) plan_from_arguments(plan);
-    Slice slice;
-    if constexpr (SPLIT) {
-        slice = slice_of_block(plan.split, 0, n_kv);
-    } else {
-        slice.wg = blockIdx.x / n_kv;
-    }
+    __shared__ __attribute__((aligned(16))) float lds[4][kFoldFloats];
+    const Slice slice = unit_of_block<SPLIT, INLINE>(plan, n_kv);
     tables_unwritten(plan);
     if ((plan.wgs[slice.wg].row_tiles & 255) == 2)
         attend_unit<2, SPLIT>(lds, slice, pool, q, plan, n_cand, n_q, n_kv, group, scale_log2e, part, cand_k, cand_v, cand_mask, out);
@@ -474,10 +524,15 @@ hipError_t launch_attention_fp4(const Shape& s, const void* pool, const void* q,
     const int64_t n = ((int64_t)n_class[1] + n_class[2]) * s.n_kv;
     if (n > 0x7fffffff || n_class[0] > 0) return hipErrorInvalidValue;  // (4-bit pools have no matrix units)
     if (n == 0) return hipSuccess;
-#define APAR_LAUNCH(SPLITV, INLINEV, WORDS)                                                                             \
-    hipLaunchKernelGGL((attention_fp4<SPLITV, INLINEV>), dim3((unsigned)n), dim3(256), 0, st, WORDS,                    \
+#define APAR_LAUNCH_KERNEL(KERNEL, WORDS)                                                                               \
+    hipLaunchKernelGGL(KERNEL, dim3((unsigned)n), dim3(256), 0, st, WORDS,                                              \
                        (const char*)pool, (const uint16_t*)q, plan, n_cand, s.n_q, s.n_kv, s.group, s.scale_log2e,      \
                        part, (const uint16_t*)cand_k, (const uint16_t*)cand_v, mask, (uint16_t*)out)
+#define APAR_LAUNCH(SPLITV, INLINEV, WORDS)                                                            \
+    do {                                                                                               \
+        if (n_class[1] == 0) APAR_LAUNCH_KERNEL((attention_fp4_one<SPLITV, INLINEV>), WORDS);          \
+        else APAR_LAUNCH_KERNEL((attention_fp4<SPLITV, INLINEV>), WORDS);                              \
+    } while (0)
     if (plan.inline_words) {
         PlanWords<true> words;
         memcpy(words.words, plan.inline_words, (size_t)plan.n_inline_words * sizeof(int32_t));
@@ -488,6 +543,7 @@ hipError_t launch_attention_fp4(const Shape& s, const void* pool, const void* q,
         APAR_LAUNCH(false, false, PlanWords<false>{});
     }
 #undef APAR_LAUNCH
+#undef APAR_LAUNCH_KERNEL
     return hipGetLastError();
 }
 

@@ -19,31 +19,43 @@ namespace apar {
 namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-template <class T>
-__device__ __forceinline__ float widened(T x);
-template <>
-__device__ __forceinline__ float widened<float>(float x) { return x; }
-template <>
-__device__ __forceinline__ float widened<uint16_t>(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
-template <class T>
-__device__ __forceinline__ T narrowed(float x);
-template <>
-__device__ __forceinline__ float narrowed<float>(float x) { return x; }
-template <>
-__device__ __forceinline__ uint16_t narrowed<uint16_t>(float x) {  // round to nearest even
-    const f32x2 p = {x, x};
-    return (uint16_t)__builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
+// W consecutive elements (16 bytes, or one) to and from floats; bf16: round to nearest even.
+__device__ __forceinline__ void load_run(const float* p, float (&x)[4]) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = v[i];
 }
+__device__ __forceinline__ void load_run(const uint16_t* p, float (&x)[8]) {
+    const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(v[i] << 16), x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+}
+__device__ __forceinline__ void load_run(const float* p, float (&x)[1]) { x[0] = *p; }
+__device__ __forceinline__ void load_run(const uint16_t* p, float (&x)[1]) { x[0] = __uint_as_float((uint32_t)*p << 16); }
+__device__ __forceinline__ uint32_t pack_pair(float lo, float hi) {
+    const f32x2 p = {lo, hi};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
+}
+__device__ __forceinline__ void store_run(float* p, const float (&x)[4]) { *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]}; }
+__device__ __forceinline__ void store_run(uint16_t* p, const float (&x)[8]) {
+    *reinterpret_cast<u32x4*>(p) = u32x4{pack_pair(x[0], x[1]), pack_pair(x[2], x[3]), pack_pair(x[4], x[5]), pack_pair(x[6], x[7])};
+}
+__device__ __forceinline__ void store_run(float* p, const float (&x)[1]) { *p = x[0]; }
+__device__ __forceinline__ void store_run(uint16_t* p, const float (&x)[1]) { *p = (uint16_t)pack_pair(x[0], x[0]); }
+
+template <class T, int W>
+struct Piece { typedef u32x4 type; };  // W elements as they are
+template <class T>
+struct Piece<T, 1> { typedef T type; };
 
 // W pairs a lane: 16 bytes of either half (1: sizes or addresses that do not allow that).  PAIRS: the dims of a pair lie side by side.
 template <class T, int W, bool PAIRS>
 __global__ __launch_bounds__(256) void rotate_rows(RotaryArgs args, RotaryCall call) {
     extern __shared__ f32x2 turns[];  // [rows of the workgroup][pairs]: cosine, sine
-    struct __attribute__((aligned(sizeof(T) * W))) Vec {
-        T x[W];
-    };
     const int64_t row0 = (int64_t)blockIdx.x * call.rows_per_wg;
     const int n_rows = (int)min((int64_t)call.rows_per_wg, call.n_rows - row0);
     const int pairs = call.rotary_dim / 2;
@@ -96,25 +108,30 @@ __global__ __launch_bounds__(256) void rotate_rows(RotaryArgs args, RotaryCall c
         T* out = (T*)x.out + (row0 + r) * x.out_stride + (int64_t)h * call.head_dim;
         if (piece >= turned) {  // dims behind the turned ones: taken over
             if (in == out) continue;
-            const Vec u = *(const Vec*)(in + 2 * W * piece), v = *(const Vec*)(in + 2 * W * piece + W);
-            *(Vec*)(out + 2 * W * piece) = u;
-            *(Vec*)(out + 2 * W * piece + W) = v;
+            typedef typename Piece<T, W>::type Bits;
+            const Bits* from = reinterpret_cast<const Bits*>(in + 2 * W * piece);
+            Bits* to = reinterpret_cast<Bits*>(out + 2 * W * piece);
+            const Bits first = from[0], second = from[1];
+            to[0] = first;
+            to[1] = second;
             continue;
         }
+        float u[W], v[W];
         const int a = PAIRS ? 2 * W * piece : W * piece, b = PAIRS ? a + W : a + pairs;
-        Vec u = *(const Vec*)(in + a), v = *(const Vec*)(in + b);
+        load_run(in + a, u);
+        load_run(in + b, v);
         const f32x2* cs = turns + r * pairs + W * piece;
 #pragma unroll
         for (int j = 0; j < W; ++j) {
             // pair j of the piece: elements j of u and of v, or 2 j and 2 j + 1 of the two together
-            T& ea = !PAIRS ? u.x[j] : 2 * j < W ? u.x[2 * j < W ? 2 * j : 0] : v.x[2 * j < W ? 0 : 2 * j - W];
-            T& eb = !PAIRS ? v.x[j] : 2 * j + 1 < W ? u.x[2 * j + 1 < W ? 2 * j + 1 : 0] : v.x[2 * j + 1 < W ? 0 : 2 * j + 1 - W];
-            const float fa = widened<T>(ea), fb = widened<T>(eb);
-            ea = narrowed<T>(fa * cs[j].x - fb * cs[j].y);
-            eb = narrowed<T>(fb * cs[j].x + fa * cs[j].y);
+            float& ea = !PAIRS ? u[j] : 2 * j < W ? u[2 * j % W] : v[2 * j % W];
+            float& eb = !PAIRS ? v[j] : 2 * j + 1 < W ? u[(2 * j + 1) % W] : v[(2 * j + 1) % W];
+            const float fa = ea, fb = eb;
+            ea = fa * cs[j].x - fb * cs[j].y;
+            eb = fb * cs[j].x + fa * cs[j].y;
         }
-        *(Vec*)(out + a) = u;
-        *(Vec*)(out + b) = v;
+        store_run(out + a, u);
+        store_run(out + b, v);
     }
 }
 

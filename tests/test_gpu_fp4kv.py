@@ -406,3 +406,24 @@ def test_a_loop_of_steps_carries_its_plan():
             ap.apar_decode_attention(pool.handle, to_dev(q, F4), live, out)
             assert_close(to_host(out), dense.decode(q, live), F4, f"step {step}")
         assert ap.apar_plan_counts(pool.handle)[1] > 10
+
+
+@pytest.mark.parametrize("group", [1, 2, 4, 8, 16])
+def test_prompts_and_segments_on_the_matrix_kernel(group):
+    """Whole prompts around block, super-block and workgroup borders, and last segments, forced onto the 32x32 kernel."""
+    t = torch()
+    rng = np.random.default_rng(40 + group)
+    n_kv = 2
+    lens = [1, 5, 16, 31, 32, 33, 64, 65, 127, 128, 129, 300]
+    w = manual_tree([-1] * len(lens) + [len(lens) - 1] * 2, lens + [40, 7], HeadConfig(n_kv * group, n_kv, 128, F4), seed=group)
+    with pool_for(w, blocks_upper_bound(w)) as pool:
+        pool.kv.fill_(0xFF)
+        dense, live = built(w, pool)
+        ap.apar_set_prefill_kernel(pool.handle, ap.APAR_PREFILL_MATRIX)
+        for m in ([dense.length(th) for th in live], [max(1, dense.length(th) // 3) for th in live], [1] * len(live)):
+            q = bf16(rng, (sum(m), n_kv * group, 128))
+            out = t.full((sum(m), n_kv * group, 128), 9.0, dtype=t.bfloat16, device="cuda:0")
+            ap.apar_prefill_attention(pool.handle, to_dev(q, F4), live, m, out)
+            assert ap.apar_last_prefill_kernel(pool.handle) == ap.APAR_PREFILL_MATRIX
+            top_v = max(np.abs(dense.rows(th)[1]).max() for th in live)
+            assert_within(to_host(out), dense.prefill(q, live, m), top_v, f"group {group}")
