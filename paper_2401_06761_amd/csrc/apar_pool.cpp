@@ -439,6 +439,9 @@ int run_append(apar_pool* p, const std::vector<int32_t>& codes, const std::vecto
 constexpr int64_t kFewAgainBytes = (int64_t)56 << 20, kFewAgainWideBytes = (int64_t)112 << 20, kFewAgainNarrowBytes = (int64_t)56 << 20;
 constexpr int64_t kFewSmallBytes = (int64_t)64 << 20;
 constexpr int32_t kFewUnits = 1024;
+// 4-bit pools: 64 requests of six threads, group 8 (1536 units) 47 -> 38 us with units of 16 rows; 24 of eight threads and five candidates (3072)
+// 55 -> 60.
+constexpr int32_t kFewUnitsFp4 = 2048;
 
 // Which units of a decode plan are cut into slices (attn_split.hpp), and the launch's workgroups in order.  A unit's cost
 // is the tiles a wavefront of it walks.  With T = total cost / shares, but at least kSliceMinTiles, units of more than T
@@ -527,6 +530,10 @@ void cut_into_slices(const PlanHost& ph, const Shape& s, bool few, size_t state_
     const int64_t shares = few ? kFewShares : s.dtype == APAR_F32 ? kSliceSharesF32 : kSliceShares;
     int64_t tiles = std::max<int64_t>(few ? kFewMinTiles : kSliceMinTiles, (total * s.n_kv + shares - 1) / shares);
     int min_gain = few ? kFewMinGain : kSliceMinGain;
+    if (s.fp4) {  // (every wavefront of a divided unit folds a quarter)
+        tiles = std::max<int64_t>(kFewMinTiles, (total * s.n_kv + kSliceShares - 1) / kSliceShares);
+        min_gain = kFewMinGain;
+    }
     if (s.dtype == APAR_F32 && ph.wgs.size() * s.n_kv <= kEstimatedUnits &&
         std::none_of(ph.wgs.begin(), ph.wgs.end(), [](const WgDesc& wg) { return wg.n_coop > 0; })) {
         std::vector<int32_t> units_of_cost((size_t)longest + 1, 0);
@@ -636,7 +643,7 @@ int decode_common(apar_pool* p, const void* q, const void* cand_k, const void* c
     prm.matrix_min_blocks = p->matrix_min_blocks;
     prm.inline_shared = p->inline_shared;
     prm.open_cost = p->reads_tiles_alone() ? 1 : kOpenTileCost;
-    prm.few_units = p->planning_set ? 0 : kFewUnits / p->shape.n_kv;
+    prm.few_units = p->planning_set ? 0 : (p->shape.fp4 ? kFewUnitsFp4 : kFewUnits) / p->shape.n_kv;
     // (wavefronts of the fp32 and 4-bit kernels read shared lists one by one: units of 16 rows read nothing more often)
     const int64_t tile_read = p->shape.n_kv * (p->shape.fp4 ? kFp4TileBytes : p->shape.fp8_sealed ? 4096 : 8192);
     prm.few_row_tiles = p->reads_tiles_alone() ? 1 : 2;

@@ -63,27 +63,25 @@ struct Row {  // the 16 rows of one tile: query operands (nearest e4m3 values, w
     float m, l;
 };
 
-struct Raw {  // a tile as this lane has it
+struct Tile {  // as this lane has it: codes, the byte of its K group's scale, the bytes of its four tokens' V scales
     u32x4 k, v;
     uint32_t ks, vs;
 };
 
-// The query operands of this lane's row; `src`: the row, or null where there is none.
-__device__ __forceinline__ void load_query(Row& st, const uint16_t* src, int g4, int c) {
+// The query operands of this lane's row; `src`: the row (any one where there is none: no branch around a load).
+__device__ __forceinline__ void load_query(Row& st, const uint16_t* src, bool ok, int g4, int c) {
+    const u32x4* p = reinterpret_cast<const u32x4*>(src + 16 * g4);
+    const u32x4 u[2][2] = {{p[0], p[1]}, {p[8], p[9]}};
     float x[2][16];
     float top[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        u32x4 u[2] = {u32x4{0u, 0u, 0u, 0u}, u32x4{0u, 0u, 0u, 0u}};
-        if (src) {
-            const u32x4* p = reinterpret_cast<const u32x4*>(src + 64 * h + 16 * g4);
-            u[0] = p[0], u[1] = p[1];
-        }
         top[h] = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            x[h][2 * i] = __uint_as_float(u[i >> 2][i & 3] << 16);
-            x[h][2 * i + 1] = __uint_as_float(u[i >> 2][i & 3] & 0xffff0000u);
+            const uint32_t w = ok ? u[h][i >> 2][i & 3] : 0u;
+            x[h][2 * i] = __uint_as_float(w << 16);
+            x[h][2 * i + 1] = __uint_as_float(w & 0xffff0000u);
             top[h] = fmaxf(top[h], fmaxf(fabsf(x[h][2 * i]), fabsf(x[h][2 * i + 1])));
         }
         top[h] = fmaxf(top[h], __shfl_xor(top[h], 16, 64));  // (dims 64 h + 32 (g / 2) .. + 31 are two lanes')
@@ -119,35 +117,11 @@ __device__ __forceinline__ void load_query(Row& st, const uint16_t* src, int g4,
     st.lo_scale = st.hi_scale - 4;
 }
 
-__device__ __forceinline__ f32x4 products(const Raw& t, const Row& st) {
+__device__ __forceinline__ f32x4 products(const Tile& t, const Row& st) {
     const i32x8 k = {(int32_t)t.k[0], (int32_t)t.k[1], (int32_t)t.k[2], (int32_t)t.k[3], 0, 0, 0, 0};
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
     s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, st.lo, s, 4, 0, 0, (int32_t)t.ks, 0, st.lo_scale);
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, st.hi, s, 4, 0, 0, (int32_t)t.ks, 0, st.hi_scale);
-}
-
-// This lane's V values of one tile: w[j][2 h + p] = tokens 4 g + 2 p, + 1 of dim 8 c + 2 j + h.
-__device__ __forceinline__ void widen(const Raw& t, uint32_t (&w)[4][4]) {
-    float s[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) s[i] = __uint_as_float(((t.vs >> (8 * i)) & 0xffu) << 23);
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
-        uint32_t a[4], b[4];
-#define APAR_WIDEN(J)                                                                                                                 \
-    a[J] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(t.v[2 * p], s[2 * p], J)),                          \
-    b[J] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(t.v[2 * p + 1], s[2 * p + 1], J))
-        APAR_WIDEN(0);
-        APAR_WIDEN(1);
-        APAR_WIDEN(2);
-        APAR_WIDEN(3);
-#undef APAR_WIDEN
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            w[j][p] = low_halves(a[j], b[j]);
-            w[j][2 + p] = high_halves(a[j], b[j]);
-        }
-    }
 }
 
 // Moves every row's reference to its running maximum where some row's logits ran away from it (its four lanes agree on it).
@@ -163,9 +137,8 @@ __device__ __forceinline__ void move_reference(Row& st, float top) {
     st.m = m_new;
 }
 
-// Two tiles' logits (-inf where this lane's row does not see the token) into one row tile's state.
-__device__ __forceinline__ void accumulate(const uint32_t (&wa)[4][4], const uint32_t (&wb)[4][4], Row& st, const f32x4& a, const f32x4& b,
-                                           float scale_log2e) {
+// Two tiles' logits (-inf where this lane's row does not see the token) -> the operand of their probabilities, added to the row's sum.
+__device__ __forceinline__ bf16x8 probabilities(Row& st, const f32x4& a, const f32x4& b, float scale_log2e) {
     const float top = fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(b[0], b[1]), fmaxf(b[2], b[3]))) * scale_log2e;
     move_reference(st, top);
     const float bias = st.m != -INFINITY ? -st.m : -INFINITY;  // (a row that has seen nothing yet)
@@ -177,11 +150,37 @@ __device__ __forceinline__ void accumulate(const uint32_t (&wa)[4][4], const uin
     }
     st.l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
     const u32x4 pw = {pack_pair(p[0], p[1]), pack_pair(p[2], p[3]), pack_pair(p[4], p[5]), pack_pair(p[6], p[7])};
-    const bf16x8 pb = __builtin_bit_cast(bf16x8, pw);
+    return __builtin_bit_cast(bf16x8, pw);
+}
+
+// This lane's V values of a tile: w[j] = tokens 4 g, + 1 and 4 g + 2, + 3 of dim 8 c + 2 j, then of the next dim.
+__device__ __forceinline__ void widen(const Tile& t, uint32_t (&w)[4][4]) {
+    float s[4];
 #pragma unroll
-    for (int jj = 0; jj < 8; ++jj) {
-        const u32x4 v = {wa[jj >> 1][2 * (jj & 1)], wa[jj >> 1][2 * (jj & 1) + 1], wb[jj >> 1][2 * (jj & 1)], wb[jj >> 1][2 * (jj & 1) + 1]};
-        st.o[jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), pb, st.o[jj], 0, 0, 0);
+    for (int i = 0; i < 4; ++i) s[i] = __uint_as_float(((t.vs >> (8 * i)) & 0xffu) << 23);
+    auto two_dims = [&](auto J) {
+        constexpr int j = decltype(J)::value;
+        uint32_t x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(t.v[i], s[i], j));
+        w[j][0] = low_halves(x[0], x[1]);
+        w[j][1] = low_halves(x[2], x[3]);
+        w[j][2] = high_halves(x[0], x[1]);
+        w[j][3] = high_halves(x[2], x[3]);
+    };
+    two_dims(std::integral_constant<int, 0>{});
+    two_dims(std::integral_constant<int, 1>{});
+    two_dims(std::integral_constant<int, 2>{});
+    two_dims(std::integral_constant<int, 3>{});
+}
+
+// O^T += V^T.P^T for a pair of tiles.
+__device__ __forceinline__ void add_values(Row& st, const bf16x8& p, const uint32_t (&wa)[4][4], const uint32_t (&wb)[4][4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const u32x4 even = {wa[j][0], wa[j][1], wb[j][0], wb[j][1]}, odd = {wa[j][2], wa[j][3], wb[j][2], wb[j][3]};
+        st.o[2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), p, st.o[2 * j], 0, 0, 0);
+        st.o[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), p, st.o[2 * j + 1], 0, 0, 0);
     }
 }
 
@@ -250,7 +249,7 @@ __device__ __forceinline__ void attend_unit(float (&lds)[4][kFoldFloats], const 
         st[nt].l = 0.0f;
 #pragma unroll
         for (int jj = 0; jj < 8; ++jj) st[nt].o[jj] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        load_query(st[nt], ok ? q + qrow * 128 : nullptr, g4, c);
+        load_query(st[nt], q + (ok ? qrow * 128 : 0), ok, g4, c);
     }
     // how many of a tile's tokens the row `ahead` row groups past its first one sees (causal tiles: one more per group)
     auto seen = [](int meta, int ahead) -> int {
@@ -259,17 +258,12 @@ __device__ __forceinline__ void attend_unit(float (&lds)[4][kFoldFloats], const 
     };
     const uint32_t k_ofs = c * 64 + g4 * 16, v_ofs = kFp4V + lane * 16;
     const uint32_t ks_ofs = kFp4KScale + c * 4 + g4, vs_ofs = kFp4VScale + g4 * 16 + (c & 12);
-    auto fetch = [&](int blk) -> Raw {
-        const char* tile = head_base + blk * block_stride;
-        Raw t;
-        t.k = *reinterpret_cast<const u32x4*>(tile + k_ofs);
-        t.v = *reinterpret_cast<const u32x4*>(tile + v_ofs);
-        t.ks = *reinterpret_cast<const uint8_t*>(tile + ks_ofs);
-        t.vs = *reinterpret_cast<const uint32_t*>(tile + vs_ofs);
-        return t;
+    auto fetch = [&](const TileRef& r) -> Tile {
+        const char* tile = head_base + r.blk * block_stride;
+        return Tile{*reinterpret_cast<const u32x4*>(tile + k_ofs), *reinterpret_cast<const u32x4*>(tile + v_ofs),
+                    *reinterpret_cast<const uint8_t*>(tile + ks_ofs), *reinterpret_cast<const uint32_t*>(tile + vs_ofs)};
     };
-    // Both lists, one after the other; `shift`: the shared list's ranges count row groups from the workgroup's first.  The words of the
-    // pair after the next one are on their way while the next one's tiles are.
+    // Both lists, one after the other; `shift`: the shared list's ranges count row groups from the workgroup's first.
     for (int list = 0; list < 2; ++list) {
         const TileRef* tiles = plan.tiles + (list == 0 ? coop_ofs : wi.tile_ofs);
         const int n = list == 0 ? n_coop : wi.n_tiles;
@@ -304,26 +298,29 @@ __device__ __forceinline__ void attend_unit(float (&lds)[4][kFoldFloats], const 
         auto whole = [&](int meta) {
             return (meta & 1023) - shift <= 0 && ((meta >> 10) & 1023) - shift >= wi.n_grp && meta >> 20 == 16;
         };
-        Pair p = next_pair();
-        if (!p.any) continue;
-        Raw ta = fetch(p.a.blk), tb = fetch(p.b.blk);
-        Pair p1 = next_pair();
+        // The next pair is fetched as soon as V is widened; the words of the pair after that are on their way too.  (With two to four pairs
+        // on their way, at two wavefronts per SIMD instead of three, calls were slower: 64 requests of group 8 38 -> 45 us, 16 long ones
+        // 30 -> 33; with V widened between the products and four wavefronts per SIMD 38 -> 40, 30 -> 34.)
+        Pair now = next_pair();
+        if (!now.any) continue;
+        Tile ta = fetch(now.a), tb = fetch(now.b);
+        Pair coming = next_pair();
         while (true) {
-            const Raw xa = fetch(p1.a.blk), xb = fetch(p1.b.blk);
-            const Pair p2 = next_pair();
             f32x4 sa[NT], sb[NT];
             uint32_t wa[4][4], wb[4][4];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) sa[nt] = products(ta, st[nt]), sb[nt] = products(tb, st[nt]);
             widen(ta, wa);
             widen(tb, wb);
-            if (!(whole(p.a.meta) && whole(p.b.meta))) {  // (rows that are none take part in whole tiles: nobody writes them)
-                const int alo = (p.a.meta & 1023) - shift, ahi = ((p.a.meta >> 10) & 1023) - shift;
-                const int blo = (p.b.meta & 1023) - shift, bhi = ((p.b.meta >> 10) & 1023) - shift;
+            ta = fetch(coming.a), tb = fetch(coming.b);
+            const Pair after = next_pair();
+            if (!(whole(now.a.meta) && whole(now.b.meta))) {  // (rows that are none take part in whole tiles: nobody writes them)
+                const int alo = (now.a.meta & 1023) - shift, ahi = ((now.a.meta >> 10) & 1023) - shift;
+                const int blo = (now.b.meta & 1023) - shift, bhi = ((now.b.meta >> 10) & 1023) - shift;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    const int mine_a = (my_j[nt] >= max(alo, 0) && my_j[nt] < ahi ? seen(p.a.meta, my_j[nt] - alo) : 0) - 4 * g4;
-                    const int mine_b = (my_j[nt] >= max(blo, 0) && my_j[nt] < bhi ? seen(p.b.meta, my_j[nt] - blo) : 0) - 4 * g4;
+                    const int mine_a = (my_j[nt] >= max(alo, 0) && my_j[nt] < ahi ? seen(now.a.meta, my_j[nt] - alo) : 0) - 4 * g4;
+                    const int mine_b = (my_j[nt] >= max(blo, 0) && my_j[nt] < bhi ? seen(now.b.meta, my_j[nt] - blo) : 0) - 4 * g4;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         sa[nt][i] = i < mine_a ? sa[nt][i] : -INFINITY;
@@ -332,70 +329,87 @@ __device__ __forceinline__ void attend_unit(float (&lds)[4][kFoldFloats], const 
                 }
             }
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) accumulate(wa, wb, st[nt], sa[nt], sb[nt], scale_log2e);
-            if (!p1.any) break;
-            p = p1, p1 = p2, ta = xa, tb = xb;
+            for (int nt = 0; nt < NT; ++nt) add_values(st[nt], probabilities(st[nt], sa[nt], sb[nt], scale_log2e), wa, wb);
+            if (!coming.any) break;
+            now = coming;
+            coming = after;
         }
     }
 
-    // A multi-candidate call's candidates: one more tile of at most 8 token rows per thread (bf16, a row every n_kv * 128 elements),
-    // each visible to the rows whose mask names it; the unit that writes the rows directly adds them.
+    // A multi-candidate call's candidates (bf16, a row every n_kv * 128 elements): tiles of as many threads' as fit sixteen slots, each
+    // visible to the rows whose mask names it; the unit that writes the rows directly adds them.  (Thread by thread, their loads wait
+    // for each other: 192 threads of one candidate 26 -> 22 us.)
     if ((wi.flags & kWaveDirect) && cand_mask != nullptr && (wave == 0 || !(wi.flags & kWaveSplit)) && slice.s == 0) {
         const int64_t tok_stride = (int64_t)n_kv * 128;
-        for (int ru = wi.grp_lo / n_sl; ru <= (wi.grp_lo + wi.n_grp - 1) / n_sl; ++ru) {
-            const int listed_u = plan.dfs_threads ? plan.dfs_threads[ru] : ru;
-            const int64_t base = ((int64_t)listed_u * n_cand * n_kv + kvh) * 128;
-            // K: dims 32 g .. + 31 of candidate c; V: dims 8 c .. + 7 of candidates 4 g + i (past the last one: the first, seen by nobody)
+        const int rank_hi = (wi.grp_lo + wi.n_grp - 1) / n_sl, threads = 16 / n_cand;
+        for (int ru = wi.grp_lo / n_sl; ru <= rank_hi; ru += threads) {
+            // where slot x's row starts (past the last candidate: the first one's, seen by nobody)
+            auto row_at = [&](int x) -> int64_t {
+                const int u = x / n_cand, rank = ru + u;
+                const bool real = u < threads && rank <= rank_hi;
+                const int from = real ? rank : ru;
+                const int listed_u = plan.dfs_threads ? plan.dfs_threads[from] : from;
+                return ((int64_t)listed_u * n_cand + (real ? x - u * n_cand : 0)) * tok_stride + kvh * 128;
+            };
+            // K: dims 32 g .. + 31 of slot c; V: dims 8 c .. + 7 of slots 4 g + i
             u32x4 ck[4], cv[4];
+            const uint16_t* k_row = cand_k + row_at(c) + 32 * g4;
             bool fine = true;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                ck[r] = *reinterpret_cast<const u32x4*>(cand_k + base + (c < n_cand ? c : 0) * tok_stride + 32 * g4 + 8 * r);
-                cv[r] = *reinterpret_cast<const u32x4*>(cand_v + base + (4 * g4 + r < n_cand ? 4 * g4 + r : 0) * tok_stride + 8 * c);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) fine = fine && (cv[r][i] & 0x7f80u) != 0x7f80u && (cv[r][i] & 0x7f800000u) != 0x7f800000u;
+                ck[r] = *reinterpret_cast<const u32x4*>(k_row + 8 * r);
+                cv[r] = *reinterpret_cast<const u32x4*>(cand_v + row_at(4 * g4 + r) + 8 * c);
             }
-            const bool all_fine = __builtin_amdgcn_ballot_w64(!fine) == 0;
-            uint32_t w[4][4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    w[j][p] = low_halves(cv[2 * p][j], cv[2 * p + 1][j]);
-                    w[j][2 + p] = high_halves(cv[2 * p][j], cv[2 * p + 1][j]);
-                }
+            uint32_t sees[NT];
+            u32x4 x[NT][4];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                uint32_t tm = 0;
                 int j, listed, cc;
                 int64_t qrow, slot;
                 const bool ok = row_of(nt, c, j, listed, cc, qrow, slot);
-                if (ok && (wi.grp_lo + j) / n_sl == ru) tm = cand_mask[(int64_t)listed_u * n_cand + cc] & ((1u << n_cand) - 1u);
-                if (__builtin_amdgcn_ballot_w64(tm != 0) == 0) continue;
+                const int u = ok ? (wi.grp_lo + j) / n_sl - ru : -1;
+                const bool here = u >= 0 && u < threads;
+                // (a row that is none: any one's mask and query; nobody looks at its products)
+                const uint32_t tm = cand_mask[here ? (int64_t)listed * n_cand + cc : 0] & ((1u << n_cand) - 1u);
+                sees[nt] = here ? tm << (u * n_cand) : 0u;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[nt][r] = *reinterpret_cast<const u32x4*>(q + (here ? qrow * 128 : 0) + 32 * g4 + 8 * r);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) fine = fine && (cv[r][i] & 0x7f80u) != 0x7f80u && (cv[r][i] & 0x7f800000u) != 0x7f800000u;
+            const bool all_fine = __builtin_amdgcn_ballot_w64(!fine) == 0;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                if (__builtin_amdgcn_ballot_w64(sees[nt] != 0) == 0) continue;
                 f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    u32x4 x = {0u, 0u, 0u, 0u};
-                    if (ok) x = *reinterpret_cast<const u32x4*>(q + qrow * 128 + 32 * g4 + 8 * r);
-                    s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ck[r]), __builtin_bit_cast(bf16x8, x), s, 0, 0, 0);
-                }
-                const uint32_t mine = tm >> (4 * g4);
+                for (int r = 0; r < 4; ++r)
+                    s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ck[r]), __builtin_bit_cast(bf16x8, x[nt][r]), s, 0, 0, 0);
+                const uint32_t mine = sees[nt] >> (4 * g4);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[i] = ((mine >> i) & 1u) ? s[i] : -INFINITY;
                 if (all_fine) {
                     const f32x4 none = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                    accumulate(w, w, st[nt], s, none, scale_log2e);
+                    const bf16x8 pb = probabilities(st[nt], s, none, scale_log2e);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const u32x4 even = {low_halves(cv[0][j], cv[1][j]), low_halves(cv[2][j], cv[3][j]), 0u, 0u};
+                        const u32x4 odd = {high_halves(cv[0][j], cv[1][j]), high_halves(cv[2][j], cv[3][j]), 0u, 0u};
+                        st[nt].o[2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), pb, st[nt].o[2 * j], 0, 0, 0);
+                        st[nt].o[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), pb, st[nt].o[2 * j + 1], 0, 0, 0);
+                    }
                     continue;
                 }
                 // one by one, each only into the rows that see it
                 move_reference(st[nt], fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])) * scale_log2e);
-                for (int cp = 0; cp < n_cand; ++cp) {
+                for (int cp = 0; cp < 16; ++cp) {
                     const float logit = __shfl(cp & 2 ? (cp & 1 ? s[3] : s[2]) : (cp & 1 ? s[1] : s[0]), (cp >> 2) * 16 + c, 64);
-                    const uint32_t row_sees = __shfl((int)tm, c, 64);  // (the four lanes of a row agree)
-                    if ((row_sees >> cp) & 1u) {
+                    if ((sees[nt] >> cp) & 1u) {  // (the four lanes of a row agree)
                         const float pr = logit == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(__builtin_fmaf(logit, scale_log2e, -st[nt].m));
                         if (g4 == 0) st[nt].l += pr;
-                        const uint16_t* vr = cand_v + base + cp * tok_stride + 32 * g4;
+                        const uint16_t* vr = cand_v + row_at(cp) + 32 * g4;
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -449,7 +463,7 @@ __device__ __forceinline__ void attend_unit(float (&lds)[4][kFoldFloats], const 
     if (NT == 1 && (wi.flags & kWaveSplit)) {
         // the four wavefronts hold the same rows over different tiles: every one folds two of the eight accumulators, of its
         // workgroup's wavefronts through LDS and then of the unit's slices.  (One wavefront folding all of the slices: one thread family of 32 k
-        // tokens, 8 kv heads, 32 slices 27.6 us a call, this way FOLD_US.)
+        // tokens, 8 kv heads, 32 slices 27.6 us a call, this way 24.6.)
         float* to = lds[wave];
 #pragma unroll
         for (int jj = 0; jj < 8; ++jj) *reinterpret_cast<f32x4*>(to + (jj * 64 + lane) * 4) = st[0].o[jj];
