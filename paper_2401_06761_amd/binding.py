@@ -372,58 +372,66 @@ def apar_rotary_frequencies(rotary) -> List[float]:
     return list(buf[: n.value])
 
 
-def _rotary_rows(x, out, n_rows: Optional[int]):
-    """A [..., heads, head_dim] tensor whose heads lie side by side; rows may be any distance apart (a slice of a wider projection)."""
+def _row_step(t) -> Tuple[int, int]:
+    """(rows, elements from row to row) of a [..., heads, head_dim] tensor whose heads lie side by side."""
+    shape, stride = t.shape, t.stride()
+    dims = len(shape)
+    if not t.is_cuda or dims < 3:
+        raise ValueError("expected GPU tensors [rows, heads, head_dim]")
+    heads, d = shape[-2], shape[-1]
+    if (d > 1 and stride[-1] != 1) or (heads > 1 and stride[-2] != d):
+        raise ValueError("the heads of a row must lie side by side")
+    n = shape[0]
+    for i in range(dims - 3):  # leading dims that are one after the other
+        n *= shape[i + 1]
+        if shape[i] > 1 and stride[i] != shape[i + 1] * stride[i + 1]:
+            raise ValueError("rows must be evenly spaced")
+    if n > 1 and stride[-3] < heads * d:
+        raise ValueError("rows must not overlap")
+    return n, (stride[-3] if n > 1 else heads * d)
+
+
+def _rotary_rows(x, out, n_rows: int):
+    """A tensor's rows, any distance apart (a slice of a wider projection), and where they go."""
     if x is None:
         if out is not None:
             raise ValueError("an output without its input")
-        return None, n_rows
-    out = x if out is None else out
-
-    def layout(t):
-        if not t.is_cuda or t.dim() < 3:
-            raise ValueError("expected GPU tensors [rows, heads, head_dim]")
-        shape, stride = t.shape, t.stride()
-        if (shape[-1] > 1 and stride[-1] != 1) or (shape[-2] > 1 and stride[-2] != shape[-1]):
-            raise ValueError("the heads of a row must lie side by side")
-        for i in range(t.dim() - 3):  # leading dims that are one after the other
-            if shape[i] > 1 and stride[i] != shape[i + 1] * stride[i + 1]:
-                raise ValueError("rows must be evenly spaced")
-        n = 1
-        for s in shape[:-2]:
-            n *= s
-        row = shape[-2] * shape[-1]
-        return n, max(stride[-3], row) if n > 1 else row
-
-    n, step = layout(x)
+        return None
+    n, step = _row_step(x)
+    if n != n_rows:
+        raise ValueError(f"{n} rows where {n_rows} are meant")
+    at = x.data_ptr()
+    if out is None or out is x:
+        return AparRotaryRows(at, at, step, step, x.shape[-2])
     if out.shape != x.shape or out.dtype != x.dtype or out.device != x.device:
         raise ValueError("the output must have its input's shape, type and device")
-    if n_rows is not None and n != n_rows:
-        raise ValueError(f"{n} rows where {n_rows} are meant")
-    if n > 1 and (x.stride(-3) < x.shape[-2] * x.shape[-1] or out.stride(-3) < x.shape[-2] * x.shape[-1]):
-        raise ValueError("rows must not overlap")
-    return AparRotaryRows(x.data_ptr(), out.data_ptr(), step, layout(out)[1], x.shape[-2]), n
+    return AparRotaryRows(at, out.data_ptr(), step, _row_step(out)[1], x.shape[-2])
 
 
 def _stream_on(t, stream) -> int:
     """The given stream, or the current one of the tensor's device."""
     if stream is not None or t is None:
         return _stream(stream)
+    if _raw_stream is None:
+        _stream(None)
     import torch
 
-    return torch._C._cuda_getCurrentRawStream(t.device.index) if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
-        torch.cuda.current_stream(t.device).cuda_stream
+    if hasattr(torch._C, "_cuda_getCurrentRawStream"):
+        return torch._C._cuda_getCurrentRawStream(t.device.index)
+    return torch.cuda.current_stream(t.device).cuda_stream
 
 
-def _rows_dtype(*tensors) -> int:
+def _rows_dtype(x, y=None) -> int:
     import torch
 
-    kinds = {t.dtype for t in tensors if t is not None}
-    if kinds == {torch.float32}:
-        return APAR_F32
-    if kinds == {torch.bfloat16}:
+    a = x.dtype if x is not None else y.dtype
+    if y is not None and y.dtype != a:
+        raise ValueError("expected tensors of one type")
+    if a == torch.bfloat16:
         return APAR_BF16
-    raise ValueError("expected float32 or bfloat16, one of them")
+    if a == torch.float32:
+        return APAR_F32
+    raise ValueError("expected float32 or bfloat16")
 
 
 def apar_rotate_rows(rotary, positions, q, k=None, q_out=None, k_out=None, transposed: bool = False, stream=None) -> None:
@@ -432,13 +440,13 @@ def apar_rotate_rows(rotary, positions, q, k=None, q_out=None, k_out=None, trans
 
     if positions.dtype != torch.int32 or positions.dim() != 1:
         raise ValueError("positions must be a 1-d int32 tensor")
-    qr, n = _rotary_rows(q, q_out, positions.shape[0])
-    kr, n = _rotary_rows(k, k_out, positions.shape[0])
-    if any(t is not None and t.device != positions.device for t in (q, k)):
-        raise ValueError("all tensors must be on one device")
-    if qr is None and kr is None:
+    if q is None and k is None:
         raise ValueError("neither q nor k")
-    _check(_L().apar_rotate_rows(rotary, _rows_dtype(q, k), _ptr(positions), positions.shape[0], qr, kr, int(bool(transposed)),
+    n, device = positions.shape[0], positions.device
+    qr, kr = _rotary_rows(q, q_out, n), _rotary_rows(k, k_out, n)
+    if (q is not None and q.device != device) or (k is not None and k.device != device):
+        raise ValueError("all tensors must be on one device")
+    _check(_L().apar_rotate_rows(rotary, _rows_dtype(q, k), _ptr(positions), n, qr, kr, int(bool(transposed)),
                                  _stream_on(positions, stream)), "apar_rotate_rows")
 
 
@@ -453,8 +461,7 @@ def apar_rotate_threads(pool, rotary, threads: Sequence[int], q, k=None, q_out=N
             raise ValueError("one m per listed thread")
         rows = int(sum(m))
     dtype = _rows_dtype(q, k) if q is not None or k is not None else APAR_BF16
-    qr, _ = _rotary_rows(q, q_out, rows)
-    kr, _ = _rotary_rows(k, k_out, rows)
+    qr, kr = _rotary_rows(q, q_out, rows), _rotary_rows(k, k_out, rows)
     if mask is not None and (mask.element_size() != 1 or mask.numel() != rows):
         raise ValueError("mask must hold one byte per candidate")
     _check(_L().apar_rotate_threads(pool, rotary, dtype, arr, marr, n, where, _ptr(mask), n_cand, qr, kr, int(bool(transposed)),

@@ -315,6 +315,8 @@ inline hipError_t copy_staged(void* dev, const void* host, size_t bytes, hipStre
 hipError_t launch_scatter_words(int32_t* words, const int32_t* pairs, int n_pairs, hipStream_t st);
 // words[i] = 0 for i < n
 hipError_t launch_clear_words(int32_t* words, int n, hipStream_t st);
+// src_codes: a slot code per row; on 4-bit pools the first row's slot, then the blocks that the rows lie in
+hipError_t launch_read_rows_fp4(const Shape& s, const void* pool, const int32_t* blocks, int n_rows, void* k_out, void* v_out, hipStream_t st);
 hipError_t launch_read_rows(const Shape& s, const void* pool, const int32_t* src_codes, int n_rows, void* k_out,
                             void* v_out, hipStream_t st);
 hipError_t launch_attention_partial(const Shape& s, const void* pool, const void* q, const PlanDev& plan, int n_cand,
@@ -333,8 +335,6 @@ hipError_t launch_attention_fp4(const Shape& s, const void* pool, const void* q,
                                 hipStream_t st);
 hipError_t launch_append_fp4(const Shape& s, void* pool, const void* k, const void* v, const int32_t* words, bool on_host,
                              int n_blocks, int n_open, int n_src, hipStream_t st);
-hipError_t launch_read_rows_fp4(const Shape& s, const void* pool, const int32_t* src_codes, int n_rows, void* k_out, void* v_out,
-                                hipStream_t st);
 hipError_t launch_prefill_fp4(const Shape& s, const void* pool, const void* q, const PrefillWg* wgs, const int32_t* tables, int n_wg,
                               void* out, hipStream_t st);
 hipError_t launch_prefill_bf16(const Shape& s, const void* pool, const void* q, const PrefillWg* wgs,

@@ -96,6 +96,7 @@ struct apar_pool {
     std::vector<apar_thread> scratch_commit_ids;
     std::vector<AppendBlock> append_blocks;
     std::vector<int32_t> append_of, append_src, append_words;
+    const std::vector<int32_t> no_copies;
     apar_plan_info last_plan{};
     PlanHost plan;  // the last plan, kept for the next call to carry over, for reuse of its storage and for inspection
     // the call that plan was made or last carried over for: its listed threads, its parameters, and how many
@@ -321,6 +322,8 @@ int writes_are_private(const apar_pool* p, const std::vector<int32_t>& codes, co
     return APAR_OK;
 }
 
+int send_blocks(apar_pool* p, const std::vector<int32_t>& copies, const void* k, const void* v, hipStream_t st);
+
 // Writes the call's rows: row i to codes[i], taken from row src_rows[i] of k, v (row i if src_rows is null), one
 // AppendBlock per block written to.  A block is written by one thread only, whose rows fill its slots in order, but the
 // thread may be listed in several places: the block's rows are contiguous in the call or get a list of source rows.
@@ -365,9 +368,16 @@ int run_append(apar_pool* p, const std::vector<int32_t>& codes, const std::vecto
     if (!copies_first)
         for (size_t i = 0; i + 1 < copies.size(); i += 2) blocks[at[copies[i + 1]]].copy_of = copies[i];
     for (const AppendBlock& b : blocks) at[b.dst] = -1;
+    return send_blocks(p, copies_first ? copies : p->no_copies, k, v, st);
+}
+
+// Launches the append that p->append_blocks and p->append_src describe.  copies: blocks to be copied before anything is written.
+int send_blocks(apar_pool* p, const std::vector<int32_t>& copies, const void* k, const void* v, hipStream_t st) {
+    std::vector<AppendBlock>& blocks = p->append_blocks;
+    std::vector<int32_t>& src = p->append_src;
     int n_open = (int)blocks.size();  // the blocks that are not sealed come first
     const size_t words = blocks.size() * 4 + src.size();
-    const size_t copy_words = copies_first ? copies.size() : 0;
+    const size_t copy_words = copies.size();
     bool inlined = words <= (size_t)kAppendInlineWords && copy_words == 0;
     if (p->shape.dtype != APAR_F32) {
         const bool fp4 = p->shape.fp4 != 0;  // (nothing is sealed: whole blocks have a kernel of their own)
@@ -1235,12 +1245,32 @@ int apar_append_kv(apar_pool* p, apar_thread thread, const void* k_dev, const vo
     int64_t need = (t->len + n_tokens + B - 1) / B - (t->len + B - 1) / B;
     if (t->len % B != 0 && p->ref[t->table.back()] > 1) need += 1;
     if (need > (int64_t)p->free_stack.size()) return APAR_ERR_OUT_OF_BLOCKS;
-    std::vector<int32_t> codes(n_tokens), copies, seals;
-    for (int i = 0; i < n_tokens; ++i) codes[i] = append_one(p, *t, copies, seals);
-    if (p->check_writes && writes_are_private(p, codes, copies, seals) != APAR_OK) return APAR_ERR_INTERNAL;
+    // Block by block what append_one does token by token: only the first of them can be a shared tail, and nothing but this thread's rows
+    // goes into any.  (Rows of 8 heads, host time of the call: 4000 rows 17.5 -> 7.0 us, 8000 27.8 -> 7.4.)
+    std::vector<AppendBlock>& blocks = p->append_blocks;
+    blocks.clear();
+    p->append_src.clear();
+    for (int row = 0; row < n_tokens;) {
+        const int slot = (int)(t->len % B), rows = std::min((int)B - slot, n_tokens - row);
+        int32_t copy_of = -1;
+        if (slot == 0) {
+            t->table.push_back(pop_block(p));
+        } else if (const int32_t tail = t->table.back(); p->ref[tail] > 1) {  // shared, partly filled tail: copy on write
+            t->table.back() = pop_block(p);
+            p->ref[tail] -= 1;
+            p->cow_copies += 1;
+            copy_of = tail;
+        }
+        blocks.push_back(AppendBlock{t->table.back(), copy_of, row, slot | (slot + rows) << 8});
+        t->len += rows;
+        row += rows;
+    }
+    if (p->check_writes)
+        for (const AppendBlock& b : blocks)
+            if (p->ref[b.dst] != 1 || b.copy_of == b.dst) return APAR_ERR_INTERNAL;
     if (p->dry_run) return APAR_OK;
     DeviceGuard guard(p->device);
-    return run_append(p, codes, copies, nullptr, k_dev, v_dev, (hipStream_t)hip_stream);
+    return send_blocks(p, p->no_copies, k_dev, v_dev, (hipStream_t)hip_stream);
 }
 
 // One row per entry of `threads` (a thread may repeat), row i taken from row src_rows[i] of k_dev, v_dev
@@ -1458,15 +1488,22 @@ int apar_read_kv_rows(apar_pool* p, apar_thread thread, int64_t first, int n, vo
     DeviceGuard guard(p->device);
     hipStream_t st = (hipStream_t)hip_stream;
     StageSlot* s = nullptr;
-    int rc = acquire_stage(p, (size_t)n * sizeof(int32_t), &s);
+    // (4-bit pools: the blocks, not a word per row)
+    const size_t words = p->shape.fp4 ? 1 + (size_t)(first % kBlockTokens + n + kBlockTokens - 1) / kBlockTokens : (size_t)n;
+    int rc = acquire_stage(p, words * sizeof(int32_t), &s);
     if (rc != APAR_OK) return rc;
     int32_t* codes = (int32_t*)s->host;
-    for (int i = 0; i < n; ++i) {
-        const int64_t pos = first + i;
-        const bool sealed = p->shape.dtype == APAR_BF16 && (pos / kBlockTokens + 1) * kBlockTokens <= t->len;
-        codes[i] = slot_code(*t, pos) | (sealed ? kCodeSealed : 0);
+    if (p->shape.fp4) {
+        codes[0] = (int32_t)(first % kBlockTokens);
+        memcpy(codes + 1, t->table.data() + first / kBlockTokens, (words - 1) * sizeof(int32_t));
+    } else {
+        for (int i = 0; i < n; ++i) {
+            const int64_t pos = first + i;
+            const bool sealed = p->shape.dtype == APAR_BF16 && (pos / kBlockTokens + 1) * kBlockTokens <= t->len;
+            codes[i] = slot_code(*t, pos) | (sealed ? kCodeSealed : 0);
+        }
     }
-    if ((rc = upload(p, s, (size_t)n * sizeof(int32_t), st)) != APAR_OK) return rc;
+    if ((rc = upload(p, s, words * sizeof(int32_t), st)) != APAR_OK) return rc;
     HIP_TRY(launch_read_rows(p->shape, p->kv, (const int32_t*)s->dev, n, k_out_dev, v_out_dev, st));
     HIP_TRY(hipEventRecord(s->ev, st));
     s->pending = true;

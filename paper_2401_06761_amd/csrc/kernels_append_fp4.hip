@@ -17,31 +17,54 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-// Magnitudes as the format holds them: beyond 6 * 2^125 = 1.5 * 2^127 (0x7f40), infinities included, as that; NaN as 0.
-__device__ __forceinline__ uint32_t held(uint32_t x) {
-    const uint32_t mag = x & 0x7fffu;
-    return mag > 0x7f80u ? 0u : (x & 0x8000u) | min(mag, 0x7f40u);
-}
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+constexpr uint32_t kMost = 0x7f407f40u;  // 6 * 2^125 = 1.5 * 2^127, the largest magnitude the format holds, as bf16, twice
 
-// Eight dims of a row, 16 bytes -> their codes; scale: the byte of the lane's group.  All lanes of a group call together.
-__device__ __forceinline__ uint32_t quantise(const u32x4& x, uint32_t& scale) {
-    uint32_t w[4], top = 0;
+// Eight values as the format holds them - magnitudes beyond 6 * 2^125, infinities included, as that; NaN as 0 -, and the largest magnitude.
+// Two values at a time; NaN have a branch.
+__device__ __forceinline__ uint32_t held_run(u32x4& x) {
+    u16x2 top = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, (uint32_t)(x[i] & 0x7fff7fffu)));
+    if (__builtin_amdgcn_ballot_w64(max(top.x, top.y) > 0x7f80) != 0) {
+        top = u16x2{0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if ((x[i] & 0x7fffu) > 0x7f80u) x[i] &= 0xffff0000u;
+            if ((x[i] & 0x7fff0000u) > 0x7f800000u) x[i] &= 0xffffu;
+            top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, (uint32_t)(x[i] & 0x7fff7fffu)));
+        }
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t lo = held(x[i] & 0xffffu), hi = held(x[i] >> 16);
-        w[i] = lo | hi << 16;
-        top = max(top, max(lo & 0x7fffu, hi & 0x7fffu));
+        const u16x2 mag = __builtin_elementwise_min(__builtin_bit_cast(u16x2, (uint32_t)(x[i] & 0x7fff7fffu)), __builtin_bit_cast(u16x2, kMost));
+        x[i] = (x[i] & 0x80008000u) | __builtin_bit_cast(uint32_t, mag);
     }
-    top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
+    return min((uint32_t)max(top.x, top.y), kMost & 0xffffu);
+}
+// The scale's byte for a group whose largest magnitude is `top`.
+__device__ __forceinline__ uint32_t scale_for(uint32_t top) {
     const int b = (int)(top >> 7) - 2 + ((top & 127u) > 64u ? 1 : 0);
-    scale = top == 0u ? 127u : (uint32_t)max(b, 7);
+    return top == 0u ? 127u : (uint32_t)max(b, 7);
+}
+__device__ __forceinline__ uint32_t codes_of(const u32x4& x, uint32_t scale) {
     const float s = __uint_as_float(scale << 23);
+    // (words of their own: a bit_cast of a vector's element takes the first one, whichever it names)
+    const uint32_t w[4] = {x[0], x[1], x[2], x[3]};
     uint32_t c = 0;
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[0]), s, 0);
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[1]), s, 1);
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[2]), s, 2);
     return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[3]), s, 3);
+}
+
+// Eight dims of a row, 16 bytes -> their codes; scale: the byte of the lane's group.  All lanes of a group call together.
+__device__ __forceinline__ uint32_t quantise(u32x4 x, uint32_t& scale) {
+    uint32_t top = held_run(x);
+    top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
+    scale = scale_for(top);
+    return codes_of(x, scale);
 }
 
 // Byte offsets in a tile of a token's word c (dims 8 c .. + 7) and of the scale of group g.
@@ -51,8 +74,8 @@ __device__ __forceinline__ int k_scale(int t, int g) { return kFp4KScale + 4 * t
 __device__ __forceinline__ int v_scale(int t, int g) { return kFp4VScale + (t >> 2) * 16 + 4 * g + (t & 3); }
 
 // FROM: where the descriptors and the source rows are (in the kernel's arguments: its first one).  The first workgroups take the
-// blocks that are written whole, a wavefront per (block, kv head): lane 16 g + c has dims 8 c .. + 7 of tokens 4 g .. + 3, so that V
-// codes leave as one contiguous KiB.  The others take the blocks that get a few rows, sixteen lanes per (block, kv head): the rows
+// blocks that are written whole, a wavefront per (block, kv head): V with dims 8 c .. + 7 of tokens 4 g .. + 3 in lane 16 g + c, K with
+// group g of token t in lane 4 t + g, so that the codes of either leave as one contiguous KiB and K's groups need no other lane.  The others take the blocks that get a few rows, sixteen lanes per (block, kv head): the rows
 // before the new ones where the block is the copy of a shared one, then the new ones.  Scales of V slots that are not written yet are
 // set to 0 when a block is begun, so that a reader may widen them.
 template <int FROM>
@@ -96,20 +119,25 @@ __global__ __launch_bounds__(256) void append_fp4(AppendTables<FROM> tables, cha
         if (at >= n_blocks - n_open) return;
         const AppendBlock b = block_at(n_open + at);
         char* tile = pool + ((int64_t)b.dst * n_kv + h) * kFp4TileBytes;
+        const int lane = threadIdx.x & 63;
         u32x4 kx[4], vx[4];
+        const char* k_row = k + (row_of(b, lane >> 2) * n_kv + h) * 256 + (lane & 3) * 64;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int64_t from = (row_of(b, 4 * g4 + i) * n_kv + h) * 256 + c * 16;
-            kx[i] = *reinterpret_cast<const u32x4*>(k + from);
-            vx[i] = *reinterpret_cast<const u32x4*>(v + from);
+            kx[i] = *reinterpret_cast<const u32x4*>(k_row + i * 16);
+            vx[i] = *reinterpret_cast<const u32x4*>(v + (row_of(b, 4 * g4 + i) * n_kv + h) * 256 + c * 16);
         }
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = max(top, held_run(kx[i]));
+        const uint32_t ks = scale_for(top);
+        *reinterpret_cast<u32x4*>(tile + lane * 16) = u32x4{codes_of(kx[0], ks), codes_of(kx[1], ks), codes_of(kx[2], ks), codes_of(kx[3], ks)};
+        *reinterpret_cast<uint8_t*>(tile + kFp4KScale + lane) = (uint8_t)ks;
         u32x4 vc;
         uint32_t vs = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             uint32_t s;
-            *reinterpret_cast<uint32_t*>(tile + k_word(4 * g4 + i, c)) = quantise(kx[i], s);
-            if ((c & 3) == 0) *reinterpret_cast<uint8_t*>(tile + k_scale(4 * g4 + i, c >> 2)) = (uint8_t)s;
             vc[i] = quantise(vx[i], s);
             vs |= s << (8 * i);
         }
@@ -150,15 +178,15 @@ __global__ __launch_bounds__(256) void append_fp4(AppendTables<FROM> tables, cha
         for (int t = s1; t < 16; ++t) *reinterpret_cast<uint8_t*>(tile + v_scale(t, c >> 2)) = 0;
 }
 
-__global__ __launch_bounds__(256) void read_rows_fp4(const char* __restrict__ pool, uint16_t* __restrict__ k, uint16_t* __restrict__ v,
-                                                     const int32_t* __restrict__ codes, int n_rows, int n_kv) {
+// words: the first row's slot, then the blocks that the rows lie in.
+__global__ __launch_bounds__(256) void read_rows_fp4(const int32_t* __restrict__ words, const char* __restrict__ pool, uint16_t* __restrict__ k,
+                                                     uint16_t* __restrict__ v, int n_rows, int n_kv) {
     const int64_t item = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);  // (row, kv head), heads fastest; sixteen lanes each
     const int64_t row = item / n_kv;
     if (row >= n_rows) return;
     const int h = (int)(item - row * n_kv), c = threadIdx.x & 15;
-    const int32_t code = codes[row] & ~kCodeSealed;
-    const int t = code & 15;
-    const char* tile = pool + ((int64_t)(code >> 4) * n_kv + h) * kFp4TileBytes;
+    const int at = words[0] + (int)row, t = at & 15;
+    const char* tile = pool + ((int64_t)words[1 + (at >> 4)] * n_kv + h) * kFp4TileBytes;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
         const uint32_t w = *reinterpret_cast<const uint32_t*>(tile + (half ? v_word(t, c) : k_word(t, c)));
@@ -205,12 +233,11 @@ hipError_t launch_append_fp4(const Shape& s, void* pool, const void* k, const vo
     return hipGetLastError();
 }
 
-hipError_t launch_read_rows_fp4(const Shape& s, const void* pool, const int32_t* src_codes, int n_rows, void* k_out, void* v_out,
-                                hipStream_t st) {
+hipError_t launch_read_rows_fp4(const Shape& s, const void* pool, const int32_t* blocks, int n_rows, void* k_out, void* v_out, hipStream_t st) {
     const int64_t grid = ((int64_t)n_rows * s.n_kv + 15) / 16;
-    if (grid > 0x7fffffff) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(read_rows_fp4, dim3((unsigned)grid), dim3(256), 0, st, (const char*)pool, (uint16_t*)k_out, (uint16_t*)v_out,
-                       src_codes, n_rows, s.n_kv);
+    if (grid > 0x7fffffff || n_rows > 0x7fffffff - 16) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(read_rows_fp4, dim3((unsigned)grid), dim3(256), 0, st, blocks, (const char*)pool, (uint16_t*)k_out, (uint16_t*)v_out,
+                       n_rows, s.n_kv);
     return hipGetLastError();
 }
 
