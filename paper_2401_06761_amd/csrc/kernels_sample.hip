@@ -15,6 +15,13 @@
 // runs, then among the 64 values of one.  The row stays in registers for the pass that looks for the token's index.  A value
 // that occurs more than 65535 times shows in the counters' sum; such a row goes through the digits.  Both ways give the same token.
 // What bounds it: memory, behind that the passes over the counters, which nothing fills where a compute unit has one row.
+// (256 rows of 128000 in 24 us, 65 MB; one row of 32000 in 12.5 us, of which 5 are a launch.)
+//
+// fp32 rows (sample_rows_f32): every token has a weight of its own.  Its mass goes into one of 8192 bins of equal width between the largest value
+// and the lightest that counts, a few tokens each where the row is dense; the tokens of the bin a target falls into become a list, and a
+// token's place in it comes from comparing all with all.  That is a pass for the range, one for the masses and one per list, where digits
+// take up to three per target and one for the index.  What bounds it: the weights' 64-bit instructions (12 and a conversion per token; the atomics beside
+// them cost no time of their own).  256 rows of 128000 in 90 us (173 through the digits), one row of 32000 in 25 us (52).
 #include <hip/hip_runtime.h>
 
 #include "apar_internal.hpp"
@@ -80,15 +87,36 @@ __device__ __forceinline__ void each(const T* row, int vocab, Take take) {
     if (tail < vocab) take(tail, value(row[tail]));
 }
 
+// Inclusive sum over the wavefront's lanes.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t from_lane(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 from_lane(u64 x) {
+    return (u64)from_lane<CTRL, ROWS>((uint32_t)x) | (u64)from_lane<CTRL, ROWS>((uint32_t)(x >> 32)) << 32;
+}
+template <class N>
+__device__ __forceinline__ N prefix_sum(N x) {
+    x += from_lane<0x111, 0xf>(x);  // row_shr 1, 2, 4, 8: within sixteen lanes
+    x += from_lane<0x112, 0xf>(x);
+    x += from_lane<0x114, 0xf>(x);
+    x += from_lane<0x118, 0xf>(x);
+    x += from_lane<0x142, 0xa>(x);  // lane 15 of a row to the next one, lane 31 to the upper half
+    x += from_lane<0x143, 0xc>(x);
+    return x;
+}
+__device__ __forceinline__ uint32_t at_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
+__device__ __forceinline__ u64 at_lane(u64 x, int lane) {
+    return (u64)at_lane((uint32_t)x, lane) | (u64)at_lane((uint32_t)(x >> 32), lane) << 32;
+}
+
 // Inclusive sums over the threads of the workgroup, in their order.
-__device__ __forceinline__ void scan(Shared& s, uint32_t& count, u64& mass) {
+template <class S>
+__device__ __forceinline__ void scan(S& s, uint32_t& count, u64& mass) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t c = __shfl_up(count, o, 64);
-        const u64 m = __shfl_up(mass, o, 64);
-        if (lane >= o) count += c, mass += m;
-    }
+    count = prefix_sum(count);
+    mass = prefix_sum(mass);
     if (lane == 63) s.wave_count[wave] = count, s.wave_mass[wave] = mass;
     __syncthreads();
     for (int w = 0; w < wave; ++w) count += s.wave_count[w], mass += s.wave_mass[w];
@@ -97,7 +125,8 @@ __device__ __forceinline__ void scan(Shared& s, uint32_t& count, u64& mass) {
 
 // The bin, from the largest down, in which the cumulated count or mass (of what lies above the bins, `above`, and the bins) reaches
 // the target; what lies above that bin.
-__device__ __forceinline__ int reach(Shared& s, const uint32_t* counts, const u64* masses, int bins, bool by_mass, u64 target,
+template <class S>
+__device__ __forceinline__ int reach(S& s, const uint32_t* counts, const u64* masses, int bins, bool by_mass, u64 target,
                                      uint32_t& above, u64& mass_above) {
     const int per = (bins + kThreads - 1) / kThreads;
     uint32_t c = 0;
@@ -310,37 +339,253 @@ __device__ void sample_by_digits(Shared& s, const SampleCall& call, int r) {
     }
 }
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void sample_rows(SampleCall call) {
-    __shared__ Shared s;
-    sample_by_digits<T>(s, call, blockIdx.x);
+// ---- f32 rows: bins of equal width, and a list ------------------------------------------------------
+constexpr int kFine = 8192, kList = 1024;
+
+// The weights of a row whose values are all finite, w = 2^n 2^(k/64) 2^y with |y| <= 1/128: the middle factor from a table, the last one from the
+// series of exp(y ln 2) up to y^5 (the next term is 4e-17).  A third of the 64-bit instructions of a weight without a table, and a row has one per token.
+struct TableWeights {
+    double top, scale, one;
+    const double* table;  // 2^(k/64)
+    __device__ __forceinline__ TableWeights(float t, float temperature, double unit, const double* powers)
+        : top(t), scale(fmin(1.4426950408889634074 / (double)temperature, 1e300)), one(unit), table(powers) {}
+    __device__ __forceinline__ double of(float x) const {
+        constexpr double kRound = 105553116266496.0;  // 1.5 2^46: a sum with it is a multiple of 1/64
+        const double t = fmax(((double)x - top) * scale, -1000.0);
+        const double q = t + kRound, y = t - (q - kRound);
+        const int k = (int)(uint32_t)__double_as_longlong(q);  // t in sixty-fourths
+        double p = 1.3333558146428443423e-3;  // ln(2)^5 / 5!, ...
+        p = __builtin_fma(p, y, 9.6181291076284771619e-3);
+        p = __builtin_fma(p, y, 5.5504108664821579953e-2);
+        p = __builtin_fma(p, y, 2.4022650695910071233e-1);
+        p = __builtin_fma(p, y, 6.9314718055994530942e-1);
+        p = __builtin_fma(p, y, 1.0);
+        p *= table[k & 63];
+        return __longlong_as_double(__double_as_longlong(p) + ((long long)(k >> 6) << 52));
+    }
+    __device__ __forceinline__ u64 whole(double w) const {
+        const double v = __builtin_fma(w, one, 0.5);
+        const uint32_t high = (uint32_t)(v * 2.3283064365386962891e-10);  // (2^-32)
+        return (u64)high << 32 | (uint32_t)__builtin_fma(-4294967296.0, (double)high, v);
+    }
+    __device__ __forceinline__ u64 units(float x) const { return whole(of(x)); }
+    __device__ __forceinline__ float logprob(float x, u64 mass) const {
+        return (float)(((double)x - top) * scale * 0.69314718055994530942 - log((double)mass / one));
+    }
+};
+
+struct Item {
+    u64 order;  // key and, the other way round, index: one token's is larger than another's that stands behind it
+    u64 units;
+};
+struct Binned {
+    u64 mass[kFine];
+    uint32_t count[kFine];       // (with top-k)
+    Item list[kList];
+    u64 list_mass[kList];        // up to and with an item
+    uint32_t list_count[kList];
+    double powers[64];
+    u64 wave_mass[kWaves], wave_all[kWaves], wave_least[kWaves];
+    float wave_top[kWaves], wave_low[kWaves];
+    uint32_t wave_count[kWaves], wave_tokens[kWaves];
+    uint32_t hit_bin, hit_count;
+    u64 hit_mass, hit_order;
+    uint32_t listed;
+};
+union RoomsF32 {
+    Shared digits;
+    Binned binned;
+};
+static_assert(sizeof(RoomsF32) <= 160 * 1024, "LDS of a compute unit");
+
+__global__ __launch_bounds__(kThreads) void sample_rows_f32(SampleCall call) {
+    __shared__ RoomsF32 rooms;
+    Binned& s = rooms.binned;
+    const int r = blockIdx.x, vocab = call.vocab;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const float* row = (const float*)call.logits + (int64_t)r * call.row_stride;
+    const int head = min(vocab, (int)((16 - ((uintptr_t)row & 15)) & 15) / 4);
+    const int n_body = (vocab - head) / 4, tail = head + n_body * 4;
+    const u32x4* body = reinterpret_cast<const u32x4*>(row + head);
+    const int edge = (int)threadIdx.x < head ? (int)threadIdx.x : tail + (int)threadIdx.x - 512;  // a head or (threads from 512 on) a tail element
+    const bool has_edge = (int)threadIdx.x < head || ((int)threadIdx.x >= 512 && edge < vocab);
+    const float edge_value = has_edge ? row[edge] : -INFINITY;
+    const apar_sample_row p = call.rows ? call.rows[r] : apar_sample_row{1.0f, 0, 1.0f, 0.0f};
+    const float u = call.uniforms[r];
+    // take(index, value) for every element of the row, in no order.  Four pieces of 16 bytes a thread are looked at while the next four are on their
+    // way (past the row's end the last one again, not looked at).
+    constexpr int kPieces = 4;
+    auto elements = [&](auto take) __attribute__((always_inline)) {
+        u32x4 x[kPieces];
+        auto fetch = [&](int at0) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) x[i] = body[min(at0 + i * kThreads, n_body - 1)];
+        };
+        if ((int)threadIdx.x < n_body) fetch(threadIdx.x);
+        for (int at0 = threadIdx.x; at0 < n_body; at0 += kPieces * kThreads) {
+            u32x4 now[kPieces];
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) now[i] = x[i];
+            fetch(at0 + kPieces * kThreads);
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int at = at0 + i * kThreads;
+                if (at >= n_body) break;
+                const uint32_t word[4] = {now[i][0], now[i][1], now[i][2], now[i][3]};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) take(head + at * 4 + j, __uint_as_float(word[j]));
+            }
+        }
+        if (has_edge) take(edge, edge_value);
+    };
+    auto order_of = [](int i, float x) -> u64 { return (u64)key_of(x) << 32 | (uint32_t)~i; };
+
+    if (!(p.temperature > 0.0f)) {  // the first token
+        u64 best = 0;  // (no token's)
+        elements([&](int i, float x) __attribute__((always_inline)) {
+            if (x > -INFINITY) best = max(best, order_of(i, x));
+        });
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) best = max(best, (u64)__shfl_xor((long long)best, o, 64));
+        if (lane == 0) s.wave_all[wave] = best;
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w) best = max(best, s.wave_all[w]);
+        if (threadIdx.x != 0) return;
+        if (best == 0) return write_none(call, r);
+        write_token(call, r, (int)~(uint32_t)best);
+        if (call.logprobs) call.logprobs[r] = 0.0f;
+        return;
+    }
+
+    // ---- the largest and the smallest value
+#pragma unroll
+    for (int i = 0; i < kFine / kThreads; ++i) s.mass[i * kThreads + threadIdx.x] = 0, s.count[i * kThreads + threadIdx.x] = 0;
+    if (threadIdx.x < 64) s.powers[threadIdx.x] = 2.0 * exp2_below_one((double)threadIdx.x / 64.0 - 1.0);
+    float top = -INFINITY, low = INFINITY;
+    elements([&](int, float x) __attribute__((always_inline)) { top = fmaxf(top, x), low = fminf(low, x); });  // (of a number and a NaN: the number)
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64)), low = fminf(low, __shfl_xor(low, o, 64));
+    if (lane == 0) s.wave_top[wave] = top, s.wave_low[wave] = low;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s.wave_top[w]), low = fminf(low, s.wave_low[w]);
+    if (top == -INFINITY) {  // nothing but -inf and NaN
+        if (threadIdx.x == 0) write_none(call, r);
+        return;
+    }
+    const TableWeights weights(top, p.temperature, unit_of(call), s.powers);
+    // A bin is a width of values below the largest one, places from 0 on; the subtraction, the product and their roundings keep the order.  What is
+    // lighter than half a unit weighs nothing, and the places need not reach that far: it stands in the last one.  (kFine - 1 - place: the largest
+    // values in the last bin.)
+    const double span = fmin((double)top - (double)low, (double)(call.weight_bits + 2) * 0.69314718055994530942 * (double)p.temperature);
+    const float per = span > 0.0 ? fminf((float)((kFine - 1) / span), 3.4028234e38f) : 0.0f;
+    auto place_of = [&](float x) -> float { return fminf((top - x) * per, (float)(kFine - 1)); };
+    const bool counted = p.top_k > 0, cut_by_weight = p.min_p > 0.0f;
+
+    bool crowded = top == INFINITY;  // or more tokens in a bin than the list holds: such a row goes through the digits
+    if (!crowded) {
+        // ---- every bin's mass
+        const double least = fmin((double)p.min_p, 1.0);
+        u64 mass = 0, mass_least = 0;
+        uint32_t n = 0;
+        elements([&](int, float x) __attribute__((always_inline)) {
+            if (!(x > -INFINITY)) return;
+            const double wd = weights.of(x);
+            const u64 w = weights.whole(wd);
+            const int b = kFine - 1 - (int)place_of(x);
+            if (w) atomicAdd(&s.mass[b], w);
+            if (counted) atomicAdd(&s.count[b], 1u), n += 1;
+            mass += w;
+            if (cut_by_weight) mass_least += wd < least ? 0 : w;
+        });
+        mass = prefix_sum(mass);
+        mass_least = prefix_sum(mass_least);
+        n = prefix_sum(n);
+        if (lane == 63) s.wave_all[wave] = mass, s.wave_least[wave] = mass_least, s.wave_tokens[wave] = n;
+        __syncthreads();
+        u64 kept_mass = 0, min_mass = 0;
+        uint32_t kept = 0;
+        for (int w = 0; w < kWaves; ++w) kept_mass += s.wave_all[w], min_mass += s.wave_least[w], kept += s.wave_tokens[w];
+
+        // The token on which the cumulated count or mass reaches a target: its bin; the bin's tokens as a list, with what lies above each of them
+        // (all against all); and the one of them.  With a small top-k the list begins at the first token: the cuts behind that one and the
+        // draw find their tokens in it.  (Lists of up to 1024 tokens from the first
+        // one: top-k of up to 1000 in 16 rows of 128000 takes 11 us longer.)
+        int listed_from = kFine, listed_to = -1;
+        struct Hit {
+            u64 order, mass;  // the token, the mass up to and with it
+        };
+        auto find = [&](bool by_mass, u64 target) __attribute__((always_inline)) -> Hit {
+            uint32_t above = 0;
+            u64 mass_above = 0;
+            const int b = reach(s, s.count, s.mass, kFine, by_mass, target, above, mass_above);
+            if (!by_mass && s.mass[b] == 0) return Hit{0, mass_above};
+            if (b < listed_from || b > listed_to) {
+                const bool from_first = counted && above + s.count[b] <= kList / 4;
+                listed_from = b;
+                listed_to = from_first ? kFine - 1 : b;
+                if (from_first) above = 0, mass_above = 0;
+                if (threadIdx.x == 0) s.listed = 0;
+                s.list_mass[threadIdx.x] = mass_above;
+                s.list_count[threadIdx.x] = above;
+                __syncthreads();
+                const float first = (float)(kFine - 1 - listed_to), end = (float)(kFine - listed_from);
+                elements([&](int i, float x) __attribute__((always_inline)) {
+                    const float at = place_of(x);
+                    if (!(at >= first && at < end)) return;
+                    if (!(x > -INFINITY)) return;
+                    const uint32_t slot = atomicAdd(&s.listed, 1u);
+                    if (slot < kList) s.list[slot].order = order_of(i, x);
+                });
+                __syncthreads();
+                const int m = (int)s.listed;
+                if (m > kList) {
+                    crowded = true;
+                    return Hit{0, 0};
+                }
+                if ((int)threadIdx.x < m) s.list[threadIdx.x].units = weights.units(value_of((uint32_t)(s.list[threadIdx.x].order >> 32)));
+                __syncthreads();
+                const int parts = kThreads / m, i = (int)threadIdx.x % m, part = (int)threadIdx.x / m;  // (a token's others in parts)
+                if (part < parts) {
+                    const int per_part = (m + parts - 1) / parts, stop = min((part + 1) * per_part, m);
+                    const u64 order = s.list[i].order;
+                    u64 sum = 0;
+                    uint32_t tokens = 0;
+#pragma unroll 4
+                    for (int j = part * per_part; j < stop; ++j) {
+                        const Item other = s.list[j];
+                        if (other.order >= order) sum += other.units, tokens += 1;
+                    }
+                    atomicAdd(&s.list_mass[i], sum);
+                    atomicAdd(&s.list_count[i], tokens);
+                }
+                __syncthreads();
+            }
+            const int t = (int)threadIdx.x;
+            if (t < (int)s.listed) {
+                const u64 units = s.list[t].units, to = by_mass ? s.list_mass[t] : s.list_count[t], before = to - (by_mass ? units : 1);
+                if (before < target && target <= to) s.hit_order = s.list[t].order, s.hit_mass = s.list_mass[t];
+            }
+            __syncthreads();
+            return Hit{s.hit_order, s.hit_mass};
+        };
+        if (counted && (uint32_t)p.top_k < kept) kept_mass = find(false, (u64)p.top_k).mass;
+        if (!crowded && p.top_p < 1.0f) kept_mass = find(true, top_p_target(p.top_p, kept_mass)).mass;
+        if (!crowded) {
+            if (cut_by_weight) kept_mass = min(kept_mass, min_mass);  // (of two prefixes the shorter one)
+            const Hit token = find(true, draw_target(u, kept_mass));
+            if (!crowded && threadIdx.x == 0) {
+                write_token(call, r, (int)~(uint32_t)token.order);
+                if (call.logprobs) call.logprobs[r] = weights.logprob(value_of((uint32_t)(token.order >> 32)), kept_mass);
+            }
+        }
+    }
+    if (crowded) {
+        __syncthreads();
+        sample_by_digits<float>(rooms.digits, call, r);
+    }
 }
 
 // ---- bf16 rows: a counter per value ---------------------------------------------------------------
-// Inclusive sum over the wavefront's lanes.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ uint32_t from_lane(uint32_t x) {
-    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
-}
-template <int CTRL, int ROWS>
-__device__ __forceinline__ u64 from_lane(u64 x) {
-    return (u64)from_lane<CTRL, ROWS>((uint32_t)x) | (u64)from_lane<CTRL, ROWS>((uint32_t)(x >> 32)) << 32;
-}
-template <class N>
-__device__ __forceinline__ N prefix_sum(N x) {
-    x += from_lane<0x111, 0xf>(x);  // row_shr 1, 2, 4, 8: within sixteen lanes
-    x += from_lane<0x112, 0xf>(x);
-    x += from_lane<0x114, 0xf>(x);
-    x += from_lane<0x118, 0xf>(x);
-    x += from_lane<0x142, 0xa>(x);  // lane 15 of a row to the next one, lane 31 to the upper half
-    x += from_lane<0x143, 0xc>(x);
-    return x;
-}
-__device__ __forceinline__ uint32_t at_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
-__device__ __forceinline__ u64 at_lane(u64 x, int lane) {
-    return (u64)at_lane((uint32_t)x, lane) | (u64)at_lane((uint32_t)(x >> 32), lane) << 32;
-}
-
 constexpr int kRuns = 1024;  // runs of 64 bit patterns: 0 .. 510 positive values, 512 .. 1021 negative ones, the others no numbers
 
 struct Counted {
@@ -659,10 +904,11 @@ __global__ __launch_bounds__(kThreads) void sample_rows_bf16(SampleCall call) {
 hipError_t launch_sample_tokens(const SampleCall& call, bool f32, hipStream_t st) {
     if (call.n <= 0) return hipSuccess;
 #define APAR_SAMPLE(KERNEL) hipLaunchKernelGGL((KERNEL), dim3((unsigned)call.n), dim3(kThreads), 0, st, call)
-    if (f32) APAR_SAMPLE(sample_rows<float>);
-    else if (call.vocab <= 4 * 8 * kThreads) APAR_SAMPLE(sample_rows_bf16<4>);
-    else if (call.vocab <= 8 * 8 * kThreads) APAR_SAMPLE(sample_rows_bf16<8>);
-    else if (call.vocab <= 16 * 8 * kThreads) APAR_SAMPLE(sample_rows_bf16<16>);
+    const int pieces = (call.vocab / 8 + kThreads - 1) / kThreads;  // of a bf16 row, per thread
+    if (f32) APAR_SAMPLE(sample_rows_f32);
+    else if (pieces <= 4) APAR_SAMPLE(sample_rows_bf16<4>);
+    else if (pieces <= 8) APAR_SAMPLE(sample_rows_bf16<8>);
+    else if (pieces <= 16) APAR_SAMPLE(sample_rows_bf16<16>);
     else APAR_SAMPLE(sample_rows_bf16<0>);
 #undef APAR_SAMPLE
     return hipGetLastError();

@@ -258,3 +258,20 @@ def test_both_ways_of_counting_agree_to_the_bit():
         u, params = rng.random(n), some_params(rng, n)
         a, b = call(x, u, params), call(x.float(), u, params)
         assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_masked_rows_and_extreme_temperatures(dtype):
+    """Masks of the type's lowest value, weights that vanish next to the largest one, temperatures at which one token or every token counts, crowds
+    of nearly equal values."""
+    t = torch()
+    rng = np.random.default_rng(16)
+    x = values(rng, 36, 9001, dtype)
+    x[::3, 2000:8000] = t.finfo(x.dtype).min
+    x[1::6] = x[1::6] * 2.0 ** -9 + 1.0  # (few values, many tokens each as bf16; a crowd as fp32)
+    x[2, 77] = 1e4
+    x[5, 77] = -1e4
+    x[8, 4] = t.finfo(x.dtype).max
+    for temperature in (1e-38, 1e-30, 1e-3, 0.05, 40.0, 1e30):
+        params = [(temperature, int(k), float(p), 0.0) for k, p in zip(rng.choice([0, 1, 7, 300, 1100, 3500], 36), rng.choice([1.0, 0.9, 0.2], 36))]
+        compare(x, rng.random(36), params)
