@@ -64,6 +64,12 @@ def make_requests(n: int, seed: int = 0, prompt_lo: int = 16, prompt_hi: int = 2
     return [Request(i, int(lens[i]), int(seed) * 1_000_003 + i) for i in range(n)]
 
 
+def uniforms(req_seed, seq_index, length) -> np.ndarray:
+    """The uniform u in [0, 1) of every listed sequence's next token."""
+    h = _mix(np.asarray(req_seed, dtype=np.int64), np.asarray(seq_index, dtype=np.int64), np.asarray(length, dtype=np.int64))
+    return (h >> np.uint64(11)).astype(np.float64) * (1.0 / (1 << 53))
+
+
 def sample_tokens(cfg: SamplerConfig, req_seed, seq_index, length, last_token, start_len, group_size) -> np.ndarray:
     """One token per listed sequence.  All arguments are equal-length integer arrays (one entry per
     unfinished sequence): its request's seed, its index in its group, its length, its last token,
