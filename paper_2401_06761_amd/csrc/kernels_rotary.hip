@@ -74,12 +74,11 @@ __global__ __launch_bounds__(256) void rotate_rows(RotaryArgs args, RotaryCall c
         } else if (call.rows_per_entry > 0) {  // as many rows for every listed thread
             const int entry = (int)(row / call.rows_per_entry);
             pos = word(entry);
-            if (call.mask) {
-                const uint32_t seen = call.mask[row] & ((1u << call.rows_per_entry) - 1u);
-                pos += __builtin_popcount(seen) - 1;  // a candidate sees its ancestors and itself
-            } else {
-                pos += row - (int64_t)entry * call.rows_per_entry;
-            }
+            const int own = (int)(row - (int64_t)entry * call.rows_per_entry);
+            if (call.mask)  // a candidate's ancestors are the others that it sees
+                pos += __builtin_popcount(call.mask[row] & ((1u << call.rows_per_entry) - 1u) & ~(1u << own));
+            else
+                pos += own;
         } else {  // the last listed thread whose first row is not behind this one
             int lo = 0, hi = call.n_entries;
             while (hi - lo > 1) {

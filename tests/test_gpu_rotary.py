@@ -185,7 +185,7 @@ def test_rows_of_listed_threads(dtype):
             ahead[x] = ahead.get(x, 0) + mi
         compare(many[:700], pos, m=ms)
         masks = np.array([[1, 3, 5, 11, 16], [1, 2, 4, 12, 28], [0xFF, 0xE1, 4, 8, 16]], dtype=np.uint8)  # bits past the fifth do not count
-        depth = [[0, 1, 1, 2, 0], [0, 0, 0, 1, 2], [4, 0, 0, 0, 0]]
+        depth = [[0, 1, 1, 2, 0], [0, 0, 0, 1, 2], [4, 1, 0, 0, 0]]  # the others it sees; one of them does not see itself
         at = [threads[0], threads[2], threads[0]]
         compare(at, [length[x] + y for x, d in zip(at, depth) for y in d], mask=t.from_numpy(masks).cuda(), n_cand=5)
 
