@@ -427,3 +427,48 @@ def test_prompts_and_segments_on_the_matrix_kernel(group):
             assert ap.apar_last_prefill_kernel(pool.handle) == ap.APAR_PREFILL_MATRIX
             top_v = max(np.abs(dense.rows(th)[1]).max() for th in live)
             assert_within(to_host(out), dense.prefill(q, live, m), top_v, f"group {group}")
+
+
+@pytest.mark.parametrize("group", [3, 5, 6, 7, 8, 11, 12, 13, 15, 16])
+def test_any_group_with_the_most_candidates(group):
+    """Groups that divide no tile, and up to eight candidates a thread.  Refused as on all pools: more than 64 query rows of one thread in a decode
+    call, prefills with groups that do not divide a row tile."""
+    t = torch()
+    rng = np.random.default_rng(5000 + group)
+    n_kv = 2
+    n_q = n_kv * group
+    w = manual_tree([-1, 0, 0, 2, 2, -1, -1, 6], [30, 16, 9, 1, 25, 3, 200, 33], HeadConfig(n_q, n_kv, 128, F4), seed=group, data_scale=0.7)
+    with pool_for(w, blocks_upper_bound(w)) as pool:
+        pool.kv.fill_(0xFF)
+        dense, live = built(w, pool)
+        top_v = max(np.abs(dense.rows(th)[1]).max() for th in live)
+        n = len(live)
+        q = bf16(rng, (n, n_q, 128))
+        out = t.full((n, n_q, 128), 9.0, dtype=t.bfloat16, device="cuda:0")
+        ap.apar_decode_attention(pool.handle, to_dev(q, F4), live, out)
+        assert_within(to_host(out), dense.decode(q, live), top_v, "decode")
+        for C in (8, 7, 3, 1):
+            q = bf16(rng, (n, C, n_q, 128), 0.7)
+            ck, cv = bf16(rng, (n, C, n_kv, 128), 0.7), bf16(rng, (n, C, n_kv, 128), 0.7)
+            masks = np.stack([mask_rows_from_parents(draw_candidate_tree(rng, C)) for _ in range(n)])
+            out = t.full((n, C, n_q, 128), 9.0, dtype=t.bfloat16, device="cuda:0")
+            call = (pool.handle, to_dev(q, F4), to_dev(ck, F4), to_dev(cv, F4), t.from_numpy(masks).cuda(), C, live, out)
+            if C * group > 64:
+                with pytest.raises(ap.AparError) as e:
+                    ap.apar_decode_attention_spec(*call)
+                assert e.value.status == -6
+                continue
+            ap.apar_decode_attention_spec(*call)
+            assert_within(to_host(out), dense.decode_spec(q, ck, cv, masks, live), max(top_v, np.abs(cv).max()), f"{C} candidates")
+        for kernel in (ap.APAR_PREFILL_ROW_TILES, ap.APAR_PREFILL_MATRIX, ap.APAR_PREFILL_AUTO):
+            m = [int(rng.integers(1, dense.length(th) + 1)) for th in live]
+            q = bf16(rng, (sum(m), n_q, 128))
+            out = t.full((sum(m), n_q, 128), 9.0, dtype=t.bfloat16, device="cuda:0")
+            ap.apar_set_prefill_kernel(pool.handle, kernel)
+            if 16 % group:
+                with pytest.raises(ap.AparError) as e:
+                    ap.apar_prefill_attention(pool.handle, to_dev(q, F4), live, m, out)
+                assert e.value.status == -6
+                continue
+            ap.apar_prefill_attention(pool.handle, to_dev(q, F4), live, m, out)
+            assert_within(to_host(out), dense.prefill(q, live, m), top_v, "prefill")
