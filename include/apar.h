@@ -337,8 +337,8 @@ APAR_API int apar_rotate_rows(const apar_rotary* rotary, int dtype, const int32_
  *   APAR_ROWS_LAST  the thread's last m[i] rows (1 .. len), as for apar_prefill_attention.
  *   n_cand > 0      candidates ([n, n_cand] rows, mask_dev as for apar_decode_attention_spec, NEXT, m NULL): a candidate lies as
  *                   many positions behind the thread's rows as it sees other candidates.
- * dtype (of the rows: APAR_F32 on fp32 pools, APAR_BF16 on the others), numbers of heads and head_dim are the pool's.  Enqueues one launch, and an upload of a word or two per thread where there
- * are more than some 250 of them.  On a dry-run pool q, k and mask_dev are NULL.
+ * dtype (of the rows: APAR_F32 on fp32 pools, APAR_BF16 on the others), numbers of heads and head_dim are the pool's.  Enqueues one launch,
+ * and an upload of a word or two per thread where there are more than some 250 of them.  On a dry-run pool q, k and mask_dev are NULL.
  * Errors: INVALID_THREAD, INVALID_ARG, UNSUPPORTED (positions or rows past 2^31), HIP.
  */
 enum { APAR_ROWS_NEXT = 0, APAR_ROWS_LAST = 1 };
@@ -588,7 +588,7 @@ APAR_API int apar_set_chunk_blocks(apar_pool* pool, int blocks_per_unit);
  * and it has at least min_blocks blocks (default 128; shorter ones are cheaper read again by every unit below,
  * see apar_set_inline_shared).
  * Matrix units are launched ahead of the other units of a call, not beside them.  min_rows = 0 keeps every unit on the row-tile kernel; (1, 1) sends every such segment
- * to the matrix kernel.  Results agree to rounding.  fp32 and fp8 pools ignore the knob. */
+ * to the matrix kernel.  Results agree to rounding.  fp32, fp8 and 4-bit pools ignore the knob. */
 APAR_API int apar_set_matrix_units(apar_pool* pool, int min_rows, int min_blocks);
 /* Tuning knob: what happens to a sharing subtree whose threads bring more query rows than one unit carries
  * (128) and whose top segment does not go to the matrix kernel.  On (default): its threads, in depth-first
@@ -604,7 +604,8 @@ APAR_API int apar_set_inline_shared(apar_pool* pool, int on);
  * most of the rows walked are walked for threads with more than 64 query rows (query tokens x q heads per kv head),
  * on bf16 pools also for large calls and where a query token attends to 1024 rows or more on average.
  * Both give the same result to rounding.
- * fp8 pools take the matrix kernel under AUTO, by the same rule, and ROW_TILES otherwise; fp32 pools ignore the knob.
+ * fp8 pools take the matrix kernel under AUTO, by the same rule, and ROW_TILES otherwise.  4-bit pools take it under AUTO for two query
+ * tokens per thread and more, and with one under groups of more than four or in small calls; fp32 pools ignore the knob.
  * apar_last_prefill_kernel tells which one the most recent call ran (0: none). */
 enum { APAR_PREFILL_AUTO = 0, APAR_PREFILL_ROW_TILES = 1, APAR_PREFILL_MATRIX = 2 };
 APAR_API int apar_set_prefill_kernel(apar_pool* pool, int which);
