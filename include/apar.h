@@ -214,7 +214,7 @@ APAR_API int apar_decode_attention(apar_pool* pool, const void* q_dev, const apa
  * (every row must have its own bit set).  Candidates' K, V are not cached by
  * this call; append the accepted ones afterwards.
  *   q_dev, out_dev : [n, n_cand, Hq, d];  cand_k_dev, cand_v_dev : [n, n_cand, Hkv, d];
- *   mask_dev : [n, n_cand] uint8;  1 <= n_cand <= 8.
+ *   mask_dev : [n, n_cand] uint8;  1 <= n_cand <= 8, and n_cand * (Hq / Hkv) <= 64 (4-bit pools: 128), UNSUPPORTED beyond.
  */
 APAR_API int apar_decode_attention_spec(apar_pool* pool, const void* q_dev, const void* cand_k_dev,
                                const void* cand_v_dev, const uint8_t* mask_dev, int n_cand,

@@ -646,6 +646,7 @@ int decode_common(apar_pool* p, const void* q, const void* cand_k, const void* c
     PlanHost& ph = p->plan;
     PlanParams prm;
     prm.rows_per_thread = n_cand * p->shape.group;
+    if (prm.rows_per_thread > (p->shape.fp4 ? 128 : 64)) return APAR_ERR_UNSUPPORTED;  // (the other kernels hold four slices of a thread)
     prm.max_unit_tiles = p->max_unit_tiles;
     prm.allow_direct = true;
     prm.fuse = true;

@@ -182,7 +182,7 @@ struct Builder {
                 if (tail_here) leave_slack(1);
             } else if (to_matrix(s)) {
                 // matrix units: whole threads, as evenly over the workgroups as they go
-                const int per_wg = kMatrixUnitMaxRows / prm.rows_per_thread;  // >= 2: rows_per_thread <= 64
+                const int per_wg = kMatrixUnitMaxRows / prm.rows_per_thread;  // >= 1
                 const int n_wg = (s.n_shr + per_wg - 1) / per_wg;
                 const int each = (s.n_shr + n_wg - 1) / n_wg;
                 for (int t0 = 0; t0 < s.n_shr; t0 += each) {
@@ -630,7 +630,7 @@ bool kernels_take(const PlanHost& ph) {
 int build_plan(const PlanThreadView* threads, int n, const int32_t* refcount, int32_t* seg_of, const PlanParams& prm,
                PlanHost& ph) {
     ph.clear();
-    if (prm.rows_per_thread < 1 || prm.rows_per_thread > 64) return APAR_ERR_UNSUPPORTED;
+    if (prm.rows_per_thread < 1 || prm.rows_per_thread > kMatrixUnitMaxRows) return APAR_ERR_UNSUPPORTED;  // (a unit holds a thread)
     Builder bld(ph, prm);
     std::vector<PlanHost::Segment>& segs = ph.segs;
 

@@ -7,6 +7,7 @@ from apar_workloads import HeadConfig, manual_tree
 from oracle import BlockLedger
 
 from harness import blocks_upper_bound, books_equal, check_plan_covers_tables, check_prefill_plan, pool_for, random_forest, replay_trace
+from test_few_units import every_row_group_once
 
 F4 = "bf16_fp4kv"
 
@@ -55,3 +56,33 @@ def test_books_and_plans(seed):
         m = [int(rng.integers(1, led.len[t] + 1)) for t in live]
         ap.apar_prefill_attention(pool.handle, None, live, m, None)
         check_prefill_plan(pool.handle, live, m, group)
+
+
+@pytest.mark.parametrize("group,C", [(16, 5), (16, 8), (13, 5), (11, 7), (9, 8)])
+def test_plans_of_threads_with_more_than_64_rows(group, C):
+    """Candidate calls of 65 to 128 query rows a thread: plans over random forests and knobs, and along a few steps; other pools refuse them."""
+    rng = np.random.default_rng(group * C)
+    for seed in range(12):
+        parents, segs = random_forest(rng, int(rng.integers(1, 5)), int(rng.integers(3, 80)))
+        w = manual_tree(parents, segs, HeadConfig(2 * group, 2, 128, F4), seed=seed)
+        with ap.Pool(2 * group, 2, 128, F4, blocks_upper_bound(w) + 400, dry_run=True) as pool:
+            if seed % 3:
+                ap.apar_set_chunk_blocks(pool.handle, int(rng.choice([1, 2, 5, 64])))
+            if seed % 4 == 1:
+                ap.apar_set_inline_shared(pool.handle, False)
+            live, _ = replay_trace(w, pool, None, dry_run=True)
+            for step in range(4):
+                ap.apar_decode_attention_spec(pool.handle, None, None, None, None, C, live, None)
+                if ap.apar_last_plan_info(pool.handle).n_units // 2 == len(live) * -(-C * group // 16):  # (a unit per slice: a call of few units)
+                    every_row_group_once(pool.handle, live, -(-C * group // 16))
+                else:
+                    check_plan_covers_tables(pool.handle, live, 2, C * group)
+                ap.apar_append_kv_batch(pool.handle, live, None, None)
+    for dtype in ("bf16", "bf16_fp8kv", "f32"):
+        with ap.Pool(16, 1, 128, dtype, 8, dry_run=True) as pool:
+            th = ap.apar_thread_create(pool.handle)
+            ap.apar_append_kv(pool.handle, th, None, None, 3)
+            ap.apar_decode_attention_spec(pool.handle, None, None, None, None, 4, [th], None)
+            with pytest.raises(ap.AparError) as e:
+                ap.apar_decode_attention_spec(pool.handle, None, None, None, None, 5, [th], None)
+            assert e.value.status == -6

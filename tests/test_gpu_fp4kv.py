@@ -431,8 +431,8 @@ def test_prompts_and_segments_on_the_matrix_kernel(group):
 
 @pytest.mark.parametrize("group", [3, 5, 6, 7, 8, 11, 12, 13, 15, 16])
 def test_any_group_with_the_most_candidates(group):
-    """Groups that divide no tile, and up to eight candidates a thread.  Refused as on all pools: more than 64 query rows of one thread in a decode
-    call, prefills with groups that do not divide a row tile."""
+    """Groups that divide no tile, and up to eight candidates a thread, 128 query rows.  Refused as on all pools: prefills with groups that do not
+    divide a row tile."""
     t = torch()
     rng = np.random.default_rng(5000 + group)
     n_kv = 2
@@ -453,11 +453,6 @@ def test_any_group_with_the_most_candidates(group):
             masks = np.stack([mask_rows_from_parents(draw_candidate_tree(rng, C)) for _ in range(n)])
             out = t.full((n, C, n_q, 128), 9.0, dtype=t.bfloat16, device="cuda:0")
             call = (pool.handle, to_dev(q, F4), to_dev(ck, F4), to_dev(cv, F4), t.from_numpy(masks).cuda(), C, live, out)
-            if C * group > 64:
-                with pytest.raises(ap.AparError) as e:
-                    ap.apar_decode_attention_spec(*call)
-                assert e.value.status == -6
-                continue
             ap.apar_decode_attention_spec(*call)
             assert_within(to_host(out), dense.decode_spec(q, ck, cv, masks, live), max(top_v, np.abs(cv).max()), f"{C} candidates")
         for kernel in (ap.APAR_PREFILL_ROW_TILES, ap.APAR_PREFILL_MATRIX, ap.APAR_PREFILL_AUTO):
@@ -472,3 +467,33 @@ def test_any_group_with_the_most_candidates(group):
                 continue
             ap.apar_prefill_attention(pool.handle, to_dev(q, F4), live, m, out)
             assert_within(to_host(out), dense.prefill(q, live, m), top_v, "prefill")
+
+
+@pytest.mark.parametrize("group,C,chunk,inline", [(16, 8, None, True), (16, 5, 2, True), (16, 7, 3, False), (11, 8, 1, False), (13, 6, None, False)])
+def test_threads_of_more_rows_than_a_wavefront_holds(group, C, chunk, inline):
+    """65 to 128 query rows of a thread, in five to eight slices, in units of their own, cut lists and partial results."""
+    t = torch()
+    rng = np.random.default_rng(group * C)
+    parents, segs = random_forest(rng, 2, 40)
+    w = manual_tree(parents, segs, HeadConfig(group, 1, 128, F4), seed=C, data_scale=0.7)
+    with pool_for(w, blocks_upper_bound(w) + 200) as pool:
+        pool.kv.fill_(0xFF)
+        if chunk:
+            ap.apar_set_chunk_blocks(pool.handle, chunk)
+        if not inline:
+            ap.apar_set_inline_shared(pool.handle, False)
+        dense, live = built(w, pool)
+        for step in range(3):  # (the second call carries the first one's plan)
+            n = len(live)
+            q, ck, cv = bf16(rng, (n, C, group, 128), 0.7), fp4.held(bf16(rng, (n, C, 1, 128), 0.7)), fp4.held(bf16(rng, (n, C, 1, 128), 0.7))
+            masks = np.stack([mask_rows_from_parents(draw_candidate_tree(rng, C)) for _ in range(n)])
+            out = t.full((n, C, group, 128), 9.0, dtype=t.bfloat16, device="cuda:0")
+            ckd, cvd = to_dev(ck, F4), to_dev(cv, F4)
+            ap.apar_decode_attention_spec(pool.handle, to_dev(q, F4), ckd, cvd, t.from_numpy(masks).cuda(), C, live, out)
+            if chunk:
+                check_plan_covers_tables(pool.handle, live, 1, C * group)
+            top_v = max(max(np.abs(dense.rows(th)[1]).max() for th in live), np.abs(cv).max())
+            assert_within(to_host(out), dense.decode_spec(q, ck, cv, masks, live), top_v, f"step {step}")
+            accept = np.array([masks[i, int(rng.integers(0, C))] for i in range(n)], dtype=np.uint8)
+            ap.apar_commit_candidates(pool.handle, live, ckd, cvd, C, accept)
+            dense.commit_candidates(live, ck, cv, accept)
