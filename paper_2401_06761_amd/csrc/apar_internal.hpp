@@ -316,7 +316,10 @@ hipError_t launch_scatter_words(int32_t* words, const int32_t* pairs, int n_pair
 // words[i] = 0 for i < n
 hipError_t launch_clear_words(int32_t* words, int n, hipStream_t st);
 // src_codes: a slot code per row; on 4-bit pools the first row's slot, then the blocks that the rows lie in
-hipError_t launch_read_rows_fp4(const Shape& s, const void* pool, const int32_t* blocks, int n_rows, void* k_out, void* v_out, hipStream_t st);
+// words: the first row's slot and the blocks the rows lie in; on the host for up to kFp4ReadHereRows rows (they travel with the kernel's
+// arguments: a prompt of 5 rows appended and read back 18 us with an upload, 14 without), else on the device
+constexpr int kFp4ReadWords = 900, kFp4ReadHereRows = (kFp4ReadWords - 2) * kBlockTokens;
+hipError_t launch_read_rows_fp4(const Shape& s, const void* pool, const int32_t* words, int n_rows, void* k_out, void* v_out, hipStream_t st);
 hipError_t launch_read_rows(const Shape& s, const void* pool, const int32_t* src_codes, int n_rows, void* k_out,
                             void* v_out, hipStream_t st);
 hipError_t launch_attention_partial(const Shape& s, const void* pool, const void* q, const PlanDev& plan, int n_cand,

@@ -103,6 +103,7 @@ struct apar_pool {
     // threads the pool had ever created by then (a thread with an id from there on was forked since)
     std::vector<apar_thread> plan_ids;
     PlanParams plan_prm{};
+    int32_t plan_few_tiles = 0;
     size_t plan_threads_then = 0;
     int64_t plan_copies_then = 0;  // copy-on-write copies the pool had made by then
     bool plan_reuse = true;
@@ -452,6 +453,10 @@ constexpr int32_t kFewUnits = 1024;
 // 4-bit pools: 64 requests of six threads, group 8 (1536 units) 47 -> 38 us with units of 16 rows; 24 of eight threads and five candidates (3072)
 // 55 -> 60.
 constexpr int32_t kFewUnitsFp4 = 2048;
+// 4-bit pools: the most tiles such units may list (kFewTiles elsewhere), whose reading again costs a quarter: two MiB of table, and one where the
+// plan goes to the static workspace of two.  69 requests of seven threads, group 16, 2 kv heads (83 k tiles listed) under the general plan / in such
+// units 116 / 53 us, 100 of 3 k to 5 k tokens (185 k) 177 / 99, 100 of five threads, 4 kv heads (173 k) 186 / 121.
+constexpr int32_t kFewTilesFp4 = 262144, kFewTilesFp4Fixed = 131072;
 
 // Which units of a decode plan are cut into slices (attn_split.hpp), and the launch's workgroups in order.  A unit's cost
 // is the tiles a wavefront of it walks.  With T = total cost / shares, but at least kSliceMinTiles, units of more than T
@@ -662,6 +667,7 @@ int decode_common(apar_pool* p, const void* q, const void* cand_k, const void* c
     prm.few_again_wide = (int32_t)(kFewAgainWideBytes / tile_read);
     prm.few_again_narrow = (int32_t)(kFewAgainNarrowBytes / tile_read);
     prm.few_small = (int32_t)(kFewSmallBytes / tile_read);
+    const int32_t few_tiles = !p->shape.fp4 ? kFewTiles : fixed ? kFewTilesFp4Fixed : kFewTilesFp4;
     prm.few_open_cost = p->shape.fp8_sealed ? 2 : 1;  // (twice the bytes of a full one)
     // Decode calls of a loop list the same threads step after step - each a few rows longer, a few replaced
     // by a thread forked from them - and the plan of the previous call then only needs its tails brought up
@@ -669,7 +675,7 @@ int decode_common(apar_pool* p, const void* q, const void* cand_k, const void* c
     // started from a copy of its parent's table as it was then or later, so "position by position the same
     // thread or one forked from it since" is all that has to hold for patch_plan to apply.
     bool carried = false;
-    if (p->plan_reuse && ph.reusable && (size_t)n == p->plan_ids.size() && prm == p->plan_prm) {
+    if (p->plan_reuse && ph.reusable && (size_t)n == p->plan_ids.size() && prm == p->plan_prm && few_tiles == p->plan_few_tiles) {
         bool same = true;
         for (int i = 0; i < n && same; ++i) {
             int32_t t = ids[i];
@@ -678,13 +684,14 @@ int decode_common(apar_pool* p, const void* q, const void* cand_k, const void* c
         }
         carried = same && patch_plan(p->views.data(), n, p->cow_copies == p->plan_copies_then, ph);
     }
-    int rc = carried ? APAR_OK : build_plan(p->views.data(), n, p->ref.data(), p->seg_of.data(), prm, ph);
+    int rc = carried ? APAR_OK : build_plan(p->views.data(), n, p->ref.data(), p->seg_of.data(), prm, ph, few_tiles);
     if (rc != APAR_OK) {
         ph.reusable = false;
         return rc;
     }
     p->plan_ids.assign(ids, ids + n);
     p->plan_prm = prm;
+    p->plan_few_tiles = few_tiles;
     p->plan_threads_then = p->threads.size();
     p->plan_copies_then = p->cow_copies;
     (carried ? p->n_plans_carried : p->n_plans_built) += 1;
@@ -1489,6 +1496,14 @@ int apar_read_kv_rows(apar_pool* p, apar_thread thread, int64_t first, int n, vo
     DeviceGuard guard(p->device);
     hipStream_t st = (hipStream_t)hip_stream;
     StageSlot* s = nullptr;
+    if (p->shape.fp4 && n <= kFp4ReadHereRows) {
+        int32_t words[kFp4ReadWords];
+        words[0] = (int32_t)(first % kBlockTokens);
+        const int64_t b0 = first / kBlockTokens;
+        memcpy(words + 1, t->table.data() + b0, (size_t)((first + n + kBlockTokens - 1) / kBlockTokens - b0) * sizeof(int32_t));
+        HIP_TRY(launch_read_rows(p->shape, p->kv, words, n, k_out_dev, v_out_dev, st));
+        return APAR_OK;
+    }
     // (4-bit pools: the blocks, not a word per row)
     const size_t words = p->shape.fp4 ? 1 + (size_t)(first % kBlockTokens + n + kBlockTokens - 1) / kBlockTokens : (size_t)n;
     int rc = acquire_stage(p, words * sizeof(int32_t), &s);

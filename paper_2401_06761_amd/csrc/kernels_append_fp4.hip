@@ -178,9 +178,20 @@ __global__ __launch_bounds__(256) void append_fp4(AppendTables<FROM> tables, cha
         for (int t = s1; t < 16; ++t) *reinterpret_cast<uint8_t*>(tile + v_scale(t, c >> 2)) = 0;
 }
 
-// words: the first row's slot, then the blocks that the rows lie in.
-__global__ __launch_bounds__(256) void read_rows_fp4(const int32_t* __restrict__ words, const char* __restrict__ pool, uint16_t* __restrict__ k,
+// The first row's slot, then the blocks that the rows lie in: on the device, or (read where they are) the first argument itself.
+struct ReadHere {
+    int32_t words[kFp4ReadWords];
+};
+struct ReadThere {
+    const int32_t* words;
+};
+template <class TABLE>
+__global__ __launch_bounds__(256) void read_rows_fp4(TABLE table, const char* __restrict__ pool, uint16_t* __restrict__ k,
                                                      uint16_t* __restrict__ v, int n_rows, int n_kv) {
+    typedef const int32_t __attribute__((address_space(4))) * Words;
+    Words words;
+    if constexpr (sizeof(TABLE) == sizeof(ReadThere)) words = (Words)table.words;
+    else words = (Words)__builtin_amdgcn_kernarg_segment_ptr();
     const int64_t item = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);  // (row, kv head), heads fastest; sixteen lanes each
     const int64_t row = item / n_kv;
     if (row >= n_rows) return;
@@ -233,11 +244,19 @@ hipError_t launch_append_fp4(const Shape& s, void* pool, const void* k, const vo
     return hipGetLastError();
 }
 
-hipError_t launch_read_rows_fp4(const Shape& s, const void* pool, const int32_t* blocks, int n_rows, void* k_out, void* v_out, hipStream_t st) {
+hipError_t launch_read_rows_fp4(const Shape& s, const void* pool, const int32_t* words, int n_rows, void* k_out, void* v_out, hipStream_t st) {
     const int64_t grid = ((int64_t)n_rows * s.n_kv + 15) / 16;
     if (grid > 0x7fffffff || n_rows > 0x7fffffff - 16) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(read_rows_fp4, dim3((unsigned)grid), dim3(256), 0, st, blocks, (const char*)pool, (uint16_t*)k_out, (uint16_t*)v_out,
-                       n_rows, s.n_kv);
+#define APAR_READ(TABLE, ARG) \
+    hipLaunchKernelGGL(read_rows_fp4<TABLE>, dim3((unsigned)grid), dim3(256), 0, st, ARG, (const char*)pool, (uint16_t*)k_out, (uint16_t*)v_out, n_rows, s.n_kv)
+    if (n_rows <= kFp4ReadHereRows) {
+        ReadHere here;
+        memcpy(here.words, words, (1 + (words[0] + (size_t)n_rows + kBlockTokens - 1) / kBlockTokens) * sizeof(int32_t));
+        APAR_READ(ReadHere, here);
+    } else {
+        APAR_READ(ReadThere, ReadThere{words});
+    }
+#undef APAR_READ
     return hipGetLastError();
 }
 

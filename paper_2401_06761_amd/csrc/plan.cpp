@@ -59,22 +59,21 @@ constexpr int B = kBlockTokens;
 
 inline int32_t make_meta(int lo, int hi, int valid) { return lo | (hi << 10) | (valid << 20); }
 
-// The most tiles that the units of a call of few units may list: half a MiB, so that such a plan fits the static workspace.  The widest
-// tree among them, in units, where more than kFewTreeThreads threads share a unit (a wider one of those is mostly short segments
-// of many threads, which units with shared lists read once).
-constexpr int64_t kFewTiles = 65536;
+// The widest tree among the units of a call of few units, in units, where more than kFewTreeThreads threads share a unit (a wider one of
+// those is mostly short segments of many threads, which units with shared lists read once).
 constexpr int kFewTreeUnits = 4, kFewTreeThreads = 4;
 
 struct Builder {
     PlanHost& ph;
     const PlanParams& prm;
+    const int32_t few_tiles;
     int n_sl, rps, cap;  // slices per thread, rows per slice, row groups per wavefront
     int few = 0;         // row tiles that units may have in a call of few units (PlanParams::few_units); 0: another call
     // per segment: first partial row it produces itself (stand-alone: n_chunks * n_shr rows; unit root
     // that is not direct: n_shr rows), and how many chunks
     std::vector<int32_t> part0, n_chunks;
 
-    Builder(PlanHost& p, const PlanParams& q) : ph(p), prm(q) {
+    Builder(PlanHost& p, const PlanParams& q, int32_t most) : ph(p), prm(q), few_tiles(most) {
         n_sl = (q.rows_per_thread + 15) / 16;
         rps = (q.rows_per_thread + n_sl - 1) / n_sl;
         cap = 16 / rps;
@@ -587,7 +586,7 @@ struct Builder {
                 if (r.n_shr * n_sl <= 4 * cap) again_narrow += (readers - 1) * s.n_blk;
                 unique += s.n_blk;
             }
-            if (tiles > kFewTiles) continue;
+            if (tiles > few_tiles) continue;
             if (few == 1 ? again <= prm.few_again
                          : again <= prm.few_again_wide && (again_narrow <= prm.few_again_narrow || unique <= prm.few_small)) return few;
         }
@@ -628,10 +627,10 @@ bool kernels_take(const PlanHost& ph) {
 }  // namespace
 
 int build_plan(const PlanThreadView* threads, int n, const int32_t* refcount, int32_t* seg_of, const PlanParams& prm,
-               PlanHost& ph) {
+               PlanHost& ph, int32_t few_tiles) {
     ph.clear();
     if (prm.rows_per_thread < 1 || prm.rows_per_thread > kMatrixUnitMaxRows) return APAR_ERR_UNSUPPORTED;  // (a unit holds a thread)
-    Builder bld(ph, prm);
+    Builder bld(ph, prm, few_tiles);
     std::vector<PlanHost::Segment>& segs = ph.segs;
 
     // 1. segments and their forest

@@ -134,9 +134,11 @@ struct PrefillThreadView {  // one listed thread of a prefill call
 int build_prefill_plan(const PrefillThreadView* threads, int n, int group, PlanHost& ph);
 
 // seg_of: pool-sized scratch, all -1 on entry and on exit.  refcount: the pool's refcounts.
+// few_tiles: the most tiles that the units of a call of few units may list (half a MiB of them, so that such a plan fits the static workspace).
 // Returns 0, or a negative apar_status.
+constexpr int32_t kFewTiles = 65536;
 int build_plan(const PlanThreadView* threads, int n, const int32_t* refcount, int32_t* seg_of, const PlanParams& prm,
-               PlanHost& ph);
+               PlanHost& ph, int32_t few_tiles = kFewTiles);
 
 // Carries the plan in `ph` over to a call that lists, position by position, the same threads as the call it
 // was built (or last patched) for - or threads forked from them since - with the same parameters; the caller

@@ -497,3 +497,21 @@ def test_threads_of_more_rows_than_a_wavefront_holds(group, C, chunk, inline):
             accept = np.array([masks[i, int(rng.integers(0, C))] for i in range(n)], dtype=np.uint8)
             ap.apar_commit_candidates(pool.handle, live, ckd, cvd, C, accept)
             dense.commit_candidates(live, ck, cv, accept)
+
+
+def test_reads_of_few_and_many_rows():
+    """Tables that travel with the arguments and such that do not; first rows inside a block; the smallest reads."""
+    t = torch()
+    rng = np.random.default_rng(6000)
+    n = 16000
+    with ap.Pool(1, 1, 128, F4, n // 16 + 8) as pool:
+        th = ap.apar_thread_create(pool.handle)
+        k, v = bf16(rng, (n, 1, 128)), bf16(rng, (n, 1, 128))
+        ap.apar_append_kv(pool.handle, th, to_dev(k, F4), to_dev(v, F4))
+        ku, vu = fp4.held(k), fp4.held(v)
+        for first, m in ((0, 1), (15, 1), (15, 2), (n - 1, 1), (7, 14368), (15, 14368), (16, 14368), (7, 14369), (3, n - 3), (0, n)):
+            ko = t.full((m + 1, 1, 128), 7.0, dtype=t.bfloat16, device="cuda:0")
+            vo = ko.clone()
+            ap.apar_read_kv_rows(pool.handle, th, first, m, ko[:m], vo[:m])
+            assert np.array_equal(to_host(ko[:m]), ku[first:first + m]) and np.array_equal(to_host(vo[:m]), vu[first:first + m]), (first, m)
+            assert (ko[m:] == 7.0).all() and (vo[m:] == 7.0).all()
