@@ -27,6 +27,10 @@
 // finite (infinities and NaN have no code), unwritten slots have finite scales (written when the block is begun), logits are
 // replaced, not biased, where a row does not see the token.  Candidates' rows are the caller's: where one is not finite, its
 // thread's are taken one by one.
+//
+// What bounds it: HBM where a tile serves few rows (256 requests of four threads, 2 k to 4 k tokens, 32/8 heads: 1.16 GB in 210 us, 5.5 TB/s, where a bare
+// read of 2176-byte tiles reaches 6.1), vector instructions behind that (181 for a pair of tiles and 16 rows, 12 matrix ones), and
+// those alone where it serves many (60 requests of five threads of 48 rows: 0.36 PFLOP/s); a short call its launch.
 #include <hip/hip_runtime.h>
 
 #include <cstring>

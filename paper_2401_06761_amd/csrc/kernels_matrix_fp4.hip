@@ -1,6 +1,7 @@
 // Prefill attention over 4-bit pools on the 32x32 matrix instructions: the walk of matrix_walk.hpp over tiles of 2176 bytes, widened to bf16
 // when they are staged.  A tile is widened once per workgroup of 128 query rows, some fifty vector instructions of one of its wavefronts; the
-// row-tile kernel (kernels_attn_fp4.hip) leaves K as it is, but widens V for every 16 or 32 rows.
+// row-tile kernel (kernels_attn_fp4.hip) leaves K as it is, but widens V for every 16 or 32 rows.  What bounds it: the matrix pipe and the walk's
+// barriers, as on bf16 pools (five prompts of 1 k to 4.5 k tokens, 32/8 heads, 0.565 TFLOP in 570 us, 0.99 PFLOP/s; on row tiles 903).
 #include <hip/hip_runtime.h>
 
 #include "matrix_walk.hpp"
