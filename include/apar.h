@@ -431,7 +431,7 @@ APAR_API int apar_group_get_info(apar_group* group, apar_group_info* out);
  *   the token drawn is the first of those kept by all three whose cumulated mass exceeds u times their mass (u in [0, 1)).
  * temperature <= 0 (or NaN): the first token, its log-probability 0.  Logits of -inf and NaN are no tokens; a row without any gives
  * APAR_TOKEN_NONE and a log-probability of -inf.  Logits of +inf share the row among them.
- * w is computed in 64 bits and held in units of 2^-(62 - ceil(log2 vocab)); masses are sums of whole numbers of those, the same for every
+ * w is computed in 64 bits and held in units of 2^-min(51, 62 - ceil(log2 vocab)); masses are sums of whole numbers of those, the same for every
  * order of addition.  A draw depends on the row, its parameters and u alone. */
 enum { APAR_TOKEN_NONE = INT32_MIN };
 typedef struct apar_sample_row { /* one row's parameters, on the device */

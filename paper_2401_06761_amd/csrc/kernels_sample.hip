@@ -6,7 +6,7 @@
 // is the place where a cumulated count or mass reaches a target, found by digits of the values' ordered bit patterns (keys), 12, 12 and
 // 8 bits: a histogram of counts and masses over the first digit, then over the next one of the values that share the first, and so
 // on; among equal values the place follows from their weight, and the index from counting them.
-// Masses are sums of whole numbers, w 2^weight_bits rounded (42 to 62 bits by the size of the vocabulary, w computed in 64): they
+// Masses are sums of whole numbers, w 2^weight_bits rounded (42 to 51 bits by the size of the vocabulary, w computed in 64): they
 // do not depend on the order of the additions, and all prefixes agree with each other.
 //
 // bf16 rows (sample_rows_bf16): there are 65536 values, and a workgroup has room to count each of them (128 KiB of LDS, a word for the
@@ -20,8 +20,8 @@
 // fp32 rows (sample_rows_f32): every token has a weight of its own.  Its mass goes into one of 8192 bins of equal width between the largest value
 // and the lightest that counts, a few tokens each where the row is dense; the tokens of the bin a target falls into become a list, and a
 // token's place in it comes from comparing all with all.  That is a pass for the range, one for the masses and one per list, where digits
-// take up to three per target and one for the index.  What bounds it: the weights' 64-bit instructions (12 and a conversion per token; the atomics beside
-// them cost no time of their own).  256 rows of 128000 in 90 us (173 through the digits), one row of 32000 in 25 us (52).
+// take up to three per target and one for the index.  What bounds it: the weights' 64-bit instructions (some fifteen per token; the atomics beside
+// them cost no time of their own).  256 rows of 128000 in 82 us (173 through the digits), one row of 32000 in 23 us (52).
 #include <hip/hip_runtime.h>
 
 #include "apar_internal.hpp"
@@ -190,13 +190,18 @@ __device__ __forceinline__ double exp2_below_one(double t) {
     return __builtin_ldexp(p, (int)n);
 }
 
+// w in whole units, to nearest even: a unit is at least 2^-51, and a sum with 2^52 has the number in its last 52 bits.
+__device__ __forceinline__ u64 whole_units(double w, double one) {
+    return (u64)__double_as_longlong(__builtin_fma(w, one, 4503599627370496.0)) & 0xfffffffffffffull;
+}
+
 // A row's weights: w = exp((x - max) / T), and in whole units.  `scale`: log2(e) / T.
 struct Weights {
     double top, scale, one;
     __device__ __forceinline__ Weights(float t, float temperature, double unit)
         : top(t), scale(1.4426950408889634074 / (double)temperature), one(unit) {}
     __device__ __forceinline__ double of(float x) const { return (double)x == top ? 1.0 : exp2_below_one(((double)x - top) * scale); }
-    __device__ __forceinline__ u64 whole(double w) const { return (u64)(w * one + 0.5); }
+    __device__ __forceinline__ u64 whole(double w) const { return whole_units(w, one); }
     __device__ __forceinline__ u64 units(float x) const { return whole(of(x)); }
     __device__ __forceinline__ float logprob(float x, u64 mass) const {
         const double z = (double)x == top ? 0.0 : ((double)x - top) * scale * 0.69314718055994530942;
@@ -363,11 +368,7 @@ struct TableWeights {
         p *= table[k & 63];
         return __longlong_as_double(__double_as_longlong(p) + ((long long)(k >> 6) << 52));
     }
-    __device__ __forceinline__ u64 whole(double w) const {
-        const double v = __builtin_fma(w, one, 0.5);
-        const uint32_t high = (uint32_t)(v * 2.3283064365386962891e-10);  // (2^-32)
-        return (u64)high << 32 | (uint32_t)__builtin_fma(-4294967296.0, (double)high, v);
-    }
+    __device__ __forceinline__ u64 whole(double w) const { return whole_units(w, one); }
     __device__ __forceinline__ u64 units(float x) const { return whole(of(x)); }
     __device__ __forceinline__ float logprob(float x, u64 mass) const {
         return (float)(((double)x - top) * scale * 0.69314718055994530942 - log((double)mass / one));
@@ -412,9 +413,9 @@ __global__ __launch_bounds__(kThreads) void sample_rows_f32(SampleCall call) {
     const float edge_value = has_edge ? row[edge] : -INFINITY;
     const apar_sample_row p = call.rows ? call.rows[r] : apar_sample_row{1.0f, 0, 1.0f, 0.0f};
     const float u = call.uniforms[r];
-    // take(index, value) for every element of the row, in no order.  Four pieces of 16 bytes a thread are looked at while the next four are on their
-    // way (past the row's end the last one again, not looked at).
-    constexpr int kPieces = 4;
+    // take(index, value) for every element of the row, in no order.  Two pieces of 16 bytes a thread are looked at while the next two are on their
+    // way (past the row's end the last one again, not looked at).  With four a call takes 1 to 3 % longer, with six 10 to 30 %.
+    constexpr int kPieces = 2;
     auto elements = [&](auto take) __attribute__((always_inline)) {
         u32x4 x[kPieces];
         auto fetch = [&](int at0) __attribute__((always_inline)) {

@@ -40,6 +40,7 @@ int apar_sample_tokens(const void* logits_dev, int dtype, int n, int vocab, int6
     call.ids = ids ? *ids : apar_token_ids{-1, -1, -1};
     call.weight_bits = 62;
     while (((int64_t)1 << (62 - call.weight_bits)) < vocab) call.weight_bits -= 1;
+    if (call.weight_bits > 51) call.weight_bits = 51;  // (whole_units)
     DeviceOf guard(logits_dev);
     HIP_TRY(launch_sample_tokens(call, dtype == APAR_F32, (hipStream_t)hip_stream));
     return APAR_OK;

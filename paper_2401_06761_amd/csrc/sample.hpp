@@ -19,7 +19,7 @@ struct SampleCall {
     float* logprobs;                  // may be null
     int32_t n, vocab;
     apar_token_ids ids;
-    int32_t weight_bits;              // a weight of 1 is 2^weight_bits, and the weights of a row add up to less than 2^63
+    int32_t weight_bits;              // at most 51: a weight of 1 is 2^weight_bits, and the weights of a row add up to less than 2^63
 };
 
 hipError_t launch_sample_tokens(const SampleCall& call, bool f32, hipStream_t st);
