@@ -3,7 +3,7 @@
 // new thread, paragraph-node bookkeeping, release on [EOS], and Restore of the
 // paragraph tree into one linear sequence.  It samples nothing: the caller runs
 // the decode step over the unfinished sequences and hands in the tokens it drew.
-// Everything here goes through the public calls of apar.h.
+// Everything here goes through the public calls of apar.h, but for the pool's shape.
 #include <algorithm>
 #include <cstring>
 #include <deque>
@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "apar.h"
+#include "pool_access.hpp"
 
 namespace {
 
@@ -371,7 +372,9 @@ int apar_server_admit(apar_server* s, const void* k_dev, const void* v_dev, int6
     int rc = apar_pool_stats(s->pool, &ps);
     if (rc != APAR_OK) return rc;
     const bool dry = k_dev == nullptr && v_dev == nullptr;
-    const int64_t row_bytes = ps.block_bytes / 16 / 2;  // one token's K (or V) row over all kv heads
+    // one token's K (or V) row over all kv heads as the caller has it (a block may hold it in fewer bytes)
+    const apar::Shape& shape = *apar::facts_of(s->pool).shape;
+    const int64_t row_bytes = (int64_t)shape.n_kv * shape.d * (shape.dtype == APAR_F32 ? 4 : 2);
     int32_t admitted = 0;
     int64_t used = 0;
     while (!s->waiting.empty() && (int)s->running.size() < s->cfg.max_running) {

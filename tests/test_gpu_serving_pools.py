@@ -1,0 +1,125 @@
+"""The serving loop over pools that hold rows in fewer bits (GPU only): what admission caches, and every step's attention against a plain
+computation in 64 bits over the rows that each sequence should hold."""
+import numpy as np
+import pytest
+
+import paper_2401_06761_amd as ap
+from apar_workloads import SamplerConfig, make_requests, quantise, sample_tokens
+from oracle import BlockLedger, DenseThreads, fp4, fp8
+from oracle.serving import ServingOracle
+from paper_2401_06761_amd.serving import ServingRun
+
+from harness import books_equal, to_dev, to_host
+from test_gpu_fp4kv import assert_within
+
+pytestmark = pytest.mark.gpu
+CFG = SamplerConfig(p_fork=0.06, p_eos=0.03, max_threads=6, min_new=10, max_len=140)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "bf16_fp8kv", "bf16_fp4kv"])
+@pytest.mark.parametrize("n_kv", [1, 2, 8])
+def test_requests_admitted_together_have_their_own_rows(dtype, n_kv):
+    import torch
+
+    lens = [5, 16, 1, 33, 100]
+    rng = np.random.default_rng(n_kv)
+    rows = "f32" if dtype == "f32" else "bf16"
+    k, v = (quantise(rng.standard_normal((sum(lens) + 3, n_kv, 128)).astype(np.float32), rows) for _ in range(2))
+    with ap.Pool(2 * n_kv, n_kv, 128, dtype, 60) as pool:
+        pool.kv.fill_(0xFF)
+        srv = ap.apar_server_create(pool.handle, 8, 0)
+        for i, n in enumerate(lens):
+            ap.apar_server_submit(srv, i, [7] * n)
+        assert ap.apar_server_admit(srv, to_dev(k, rows), to_dev(v, rows), len(k)) == (len(lens), sum(lens))
+        at = 0
+        for e, n in zip(ap.apar_server_batch(srv), lens):
+            got = [torch.empty((n, n_kv, 128), dtype=pool.torch_dtype, device="cuda:0") for _ in range(2)]
+            ap.apar_read_kv_rows(pool.handle, int(e["thread"]), 0, n, *got)
+            torch.cuda.synchronize()
+            mine = k[at:at + n], v[at:at + n]
+            want = fp8.cached_rows(*mine) if dtype == "bf16_fp8kv" else [fp4.held(x) for x in mine] if dtype == "bf16_fp4kv" else mine
+            for g, w in zip(got, want):
+                assert np.array_equal(to_host(g), w), (int(e["request_id"]), n)
+            at += n
+        ap.apar_server_destroy(srv)
+
+
+@pytest.mark.parametrize("dtype", ["bf16_fp4kv", "bf16_fp8kv"])
+@pytest.mark.parametrize("n_blocks,max_running", [(2048, 8), (40, 6)])
+@pytest.mark.parametrize("drawn", [False, True])
+def test_serving_loop_attention_and_books(dtype, n_blocks, max_running, drawn):
+    """Outputs are held to test_gpu_fp4kv's bound: what a pool rounds is rounded in the plain computation too (fp8: rows on its grid).
+    drawn: the tokens are drawn from logits of the outputs (test_gpu_model_loop checks the draws)."""
+    import torch
+
+    n_q, n_kv, d = 4, 2, 128
+    reqs = make_requests(8, seed=5, prompt_lo=8, prompt_hi=60)
+    rng = np.random.default_rng(0)
+    qb = quantise(rng.standard_normal((64, n_q, d)).astype(np.float32), "bf16")
+    kb, vb = (quantise(rng.standard_normal((512, n_kv, d)).astype(np.float32), dtype, kv=True) for _ in range(2))
+    kh, vh = (fp4.held(x) for x in (kb, vb)) if dtype == "bf16_fp4kv" else (kb, vb)
+    pool = ap.Pool(n_q, n_kv, d, dtype, n_blocks, max_threads=1 << 20)
+    pool.kv.fill_(0xFF)
+    how = {}
+    if drawn:
+        head = to_dev((0.2 * rng.standard_normal((n_q * d, 211))).astype(np.float32), "f32")
+        bias = torch.zeros(211, device="cuda:0")
+        bias[200], bias[202] = 3.0, 2.0
+        how = dict(logits=lambda batch, out: out.float().view(len(batch), -1) @ head + bias, token_ids=(200, 201, 202), cuts=(0.9, 100, 0.95, 0.001))
+    run = ServingRun(pool, reqs, CFG, max_running, 1, banks=(to_dev(qb, "bf16"), to_dev(kb, "bf16"), to_dev(vb, "bf16")), **how)
+    run.keep_trace = True
+    led = BlockLedger(n_blocks, max_threads=1 << 20)
+    o = ServingOracle(led, max_running, 1)
+    dense = DenseThreads(n_q, n_kv, d)
+    by = {r.rid: r for r in reqs}
+    for r in reqs:
+        o.submit(r.rid, r.prompt_tokens())
+    most_admitted = steps = 0
+
+    def new_ids_up_to(tid):  # ids of children whose step was undone
+        while dense._next < tid:
+            dense.free(dense.create())
+
+    while True:
+        before = len(o.running)
+        o.admit()
+        most_admitted = max(most_admitted, len(o.running) - before)
+        used = 0
+        for r in o.running[before:]:
+            n = len(r["prompt"])
+            new_ids_up_to(r["tid"][0])
+            assert dense.create() == r["tid"][0]
+            dense.append(r["tid"][0], kh[used:used + n], vh[used:used + n])
+            used += n
+        b = o.batch()
+        more = run.step()
+        if not b:
+            assert not more
+            break
+        assert more
+        torch.cuda.synchronize()
+        assert_within(to_host(run.out[:len(b)]), dense.decode(qb[:len(b)], [e["thread"] for e in b]), np.abs(vh).max(), f"step {steps}")
+        xs = sample_tokens(CFG, [by[e["request_id"]].seed for e in b], *([e[f] for e in b] for f in
+                           ("seq_index", "length", "last_token", "start_len", "group_size"))).tolist()
+        assert run.trace[-1]["threads"] == [e["thread"] for e in b] and (drawn or run.trace[-1]["sampled"] == xs)
+        xs = run.trace[-1]["sampled"]
+        rows = np.cumsum([0] + [len(r["g"].unfinished()) + sum(s.last_token == -1 for s in r["g"].unfinished()) for r in o.running])
+        ran = list(o.running)
+        info = o.step(xs)
+        for r in ran[len(ran) - info["n_preempted"]:]:
+            for s in r["g"].unfinished():
+                dense.free(r["tid"][s.sid])
+        for parent, child in info["forks"]:
+            new_ids_up_to(child)
+            assert dense.fork(parent, 1) == [child]
+        for (ri, i), t in zip(info["rows"], info["row_threads"]):
+            at = int(rows[ri]) + i
+            dense.append(t, kh[at:at + 1], vh[at:at + 1])
+        for t in info["freed"]:
+            dense.free(t)
+        books_equal(pool.handle, led)
+        steps += 1
+    assert most_admitted > 2 and run.outputs == {rid: toks for rid, toks, _ in o.finished}
+    assert (o.preemptions > 0) == (n_blocks < 100) and sum(t["n_forked"] for t in run.trace) > 0
+    run.close()
+    pool.close()
