@@ -321,6 +321,7 @@ typedef struct apar_rotary_rows {
     void* out_dev;
     int64_t in_stride, out_stride; /* at least n_heads * head_dim */
     int32_t n_heads;
+    int32_t head_dim;              /* elements of a head of these rows: INVALID_ARG unless it is the rotary's (0: not said) */
 } apar_rotary_rows;
 APAR_API int apar_rotary_create(const apar_rotary_config* cfg, apar_rotary** out);
 APAR_API int apar_rotary_destroy(apar_rotary* rotary); /* NULL is accepted */

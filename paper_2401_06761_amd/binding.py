@@ -78,7 +78,7 @@ class AparRotaryConfig(C.Structure):
 
 class AparRotaryRows(C.Structure):
     _fields_ = [("in_dev", C.c_void_p), ("out_dev", C.c_void_p), ("in_stride", C.c_int64), ("out_stride", C.c_int64),
-                ("n_heads", C.c_int32)]
+                ("n_heads", C.c_int32), ("head_dim", C.c_int32)]
 
 
 class AparTokenIds(C.Structure):
@@ -402,10 +402,10 @@ def _rotary_rows(x, out, n_rows: int):
         raise ValueError(f"{n} rows where {n_rows} are meant")
     at = x.data_ptr()
     if out is None or out is x:
-        return AparRotaryRows(at, at, step, step, x.shape[-2])
+        return AparRotaryRows(at, at, step, step, *x.shape[-2:])
     if out.shape != x.shape or out.dtype != x.dtype or out.device != x.device:
         raise ValueError("the output must have its input's shape, type and device")
-    return AparRotaryRows(at, out.data_ptr(), step, _row_step(out)[1], x.shape[-2])
+    return AparRotaryRows(at, out.data_ptr(), step, _row_step(out)[1], *x.shape[-2:])
 
 
 def _stream_on(t, stream) -> int:

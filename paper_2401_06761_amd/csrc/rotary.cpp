@@ -19,6 +19,7 @@ namespace {
 int rotary_rows(const apar_rotary& r, const apar_rotary_rows* x, RotaryRows& out) {
     out = RotaryRows{};
     if (!x) return APAR_OK;
+    if (x->head_dim != 0 && x->head_dim != r.cfg.head_dim) return APAR_ERR_INVALID_ARG;
     const int64_t row = (int64_t)x->n_heads * r.cfg.head_dim;
     if (!x->in_dev || !x->out_dev || x->n_heads < 1 || x->in_stride < row || x->out_stride < row) return APAR_ERR_INVALID_ARG;
     if (x->in_dev == x->out_dev && x->in_stride != x->out_stride) return APAR_ERR_INVALID_ARG;
