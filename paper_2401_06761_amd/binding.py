@@ -375,20 +375,23 @@ def apar_rotary_frequencies(rotary) -> List[float]:
 def _row_step(t) -> Tuple[int, int]:
     """(rows, elements from row to row) of a [..., heads, head_dim] tensor whose heads lie side by side."""
     shape, stride = t.shape, t.stride()
-    dims = len(shape)
-    if not t.is_cuda or dims < 3:
+    if not t.is_cuda or len(shape) < 3:
         raise ValueError("expected GPU tensors [rows, heads, head_dim]")
     heads, d = shape[-2], shape[-1]
     if (d > 1 and stride[-1] != 1) or (heads > 1 and stride[-2] != d):
         raise ValueError("the heads of a row must lie side by side")
-    n = shape[0]
-    for i in range(dims - 3):  # leading dims that are one after the other
-        n *= shape[i + 1]
-        if shape[i] > 1 and stride[i] != shape[i + 1] * stride[i + 1]:
+    n, step = 1, heads * d
+    for size, apart in zip(shape[-3::-1], stride[-3::-1]):  # leading dims, the last one first; one of size 1 has no say
+        if size == 1:
+            continue
+        if n == 1:
+            step = apart
+        elif n > 0 and size > 0 and apart != n * step:
             raise ValueError("rows must be evenly spaced")
-    if n > 1 and stride[-3] < heads * d:
+        n *= size
+    if n > 1 and step < heads * d:
         raise ValueError("rows must not overlap")
-    return n, (stride[-3] if n > 1 else heads * d)
+    return n, (step if n > 1 else heads * d)
 
 
 def _rotary_rows(x, out, n_rows: int):

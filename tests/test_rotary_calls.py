@@ -47,3 +47,22 @@ def test_rows_carry_their_heads():
     rows = ap.binding._rotary_rows(OnGpu(torch.zeros(5, 6, 32)[:, 2:5]), None, 5)
     assert (rows.n_heads, rows.head_dim, rows.in_stride, rows.out_stride) == (3, 32, 192, 192)
     assert ap.AparRotaryRows(1, 1, 2, 2, 3).head_dim == 0
+
+
+def test_rows_behind_dims_of_size_one():
+    """One candidate a thread out of a wider projection, and other leading dims that say nothing."""
+    step = ap.binding._row_step
+    x = torch.zeros(7, 5, 6, 32)
+    assert step(OnGpu(x[:, :1, :2])) == (7, 5 * 6 * 32)
+    assert step(OnGpu(x[:, 2, 1:4][:, None])) == (7, 5 * 6 * 32)
+    assert step(OnGpu(x[:, None])) == (35, 6 * 32) and step(OnGpu(x[None, :, :, None, :3])) == (35, 6 * 32)
+    assert step(OnGpu(x[:1, :, :3])) == (5, 6 * 32) and step(OnGpu(x[:1, :1])) == (1, 6 * 32)
+    assert step(OnGpu(x[:, 2, :3][None].transpose(0, 1))) == (7, 5 * 6 * 32)
+    for empty in (x[:0], x[:, :0], x[:0, :, None]):
+        assert step(OnGpu(empty))[0] == 0
+    # a dim of size one says nothing of the ones around it
+    flat = torch.zeros(4096)
+    for bad in (flat.as_strided((2, 1, 3, 2, 32), (1000, 1000, 64, 32, 1)), flat.as_strided((2, 1, 3, 2, 32), (192, 192, 100, 32, 1)), x[:, :3],
+                x[:, :3, None], flat.as_strided((3, 1, 2, 32), (60, 60, 32, 1))):
+        with pytest.raises(ValueError):
+            step(OnGpu(bad))
