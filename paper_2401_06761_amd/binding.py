@@ -467,8 +467,11 @@ def apar_rotate_threads(pool, rotary, threads: Sequence[int], q, k=None, q_out=N
     qr, kr = _rotary_rows(q, q_out, rows), _rotary_rows(k, k_out, rows)
     if mask is not None and (mask.element_size() != 1 or mask.numel() != rows):
         raise ValueError("mask must hold one byte per candidate")
+    one = q if q is not None else k
+    if one is not None and ((k is not None and k.device != one.device) or (mask is not None and mask.device != one.device)):
+        raise ValueError("all tensors must be on one device")
     _check(_L().apar_rotate_threads(pool, rotary, dtype, arr, marr, n, where, _ptr(mask), n_cand, qr, kr, int(bool(transposed)),
-                                    _stream_on(q if q is not None else k, stream)), "apar_rotate_threads")
+                                    _stream_on(one, stream)), "apar_rotate_threads")
 
 
 def apar_free_thread(pool, thread: int) -> None:

@@ -66,3 +66,17 @@ def test_rows_behind_dims_of_size_one():
                 x[:, :3, None], flat.as_strided((3, 1, 2, 32), (60, 60, 32, 1))):
         with pytest.raises(ValueError):
             step(OnGpu(bad))
+
+
+def test_tensors_of_several_devices_are_refused():
+    x, y = torch.zeros(3, 4, 128), torch.zeros(3, 2, 128)
+    masks = torch.ones(3, 1, dtype=torch.uint8)
+    with ap.Pool(4, 2, 128, "f32", 8, dry_run=True) as pool, ap.Rotary(128) as rot:
+        th = [ap.apar_thread_create(pool.handle) for _ in range(3)]
+        for bad in (lambda: ap.apar_rotate_threads(pool.handle, rot.handle, th, OnGpu(x), OnGpu(y, "cuda:1"), stream=0),
+                    lambda: ap.apar_rotate_threads(pool.handle, rot.handle, th, OnGpu(x), OnGpu(y), mask=OnGpu(masks, "cuda:1"), n_cand=1, stream=0),
+                    lambda: ap.apar_rotate_threads(pool.handle, rot.handle, th, None, OnGpu(y), mask=OnGpu(masks, "cuda:1"), n_cand=1, stream=0),
+                    lambda: ap.apar_rotate_threads(pool.handle, rot.handle, th, OnGpu(x), OnGpu(y), OnGpu(x, "cuda:1"), stream=0),
+                    lambda: ap.apar_rotate_rows(rot.handle, positions(3), OnGpu(x), OnGpu(y, "cuda:1"), stream=0)):
+            with pytest.raises(ValueError):
+                bad()
