@@ -339,7 +339,8 @@ APAR_API int apar_rotate_rows(const apar_rotary* rotary, int dtype, const int32_
  *   n_cand > 0      candidates ([n, n_cand] rows, mask_dev as for apar_decode_attention_spec, NEXT, m NULL): a candidate lies as
  *                   many positions behind the thread's rows as it sees other candidates.
  * dtype (of the rows: APAR_F32 on fp32 pools, APAR_BF16 on the others), numbers of heads and head_dim are the pool's.  Enqueues one launch,
- * and an upload of a word or two per thread where there are more than some 250 of them.  On a dry-run pool q, k and mask_dev are NULL.
+ * and an upload of a word or two per thread where there are more than some 250 of them.  On a dry-run pool q, k and mask_dev are NULL
+ * and dtype says nothing.
  * Errors: INVALID_THREAD, INVALID_ARG, UNSUPPORTED (positions or rows past 2^31), HIP.
  */
 enum { APAR_ROWS_NEXT = 0, APAR_ROWS_LAST = 1 };

@@ -87,7 +87,7 @@ int rotate_threads(apar_pool* p, const apar_rotary* r, int dtype, const apar_thr
                    void* hip_stream) {
     if (!p || !r || n < 0 || (where != APAR_ROWS_NEXT && where != APAR_ROWS_LAST)) return APAR_ERR_INVALID_ARG;
     const PoolFacts pool = facts_of(p);
-    if (r->cfg.head_dim != pool.shape->d || dtype != pool.shape->dtype) return APAR_ERR_INVALID_ARG;
+    if (r->cfg.head_dim != pool.shape->d || (!pool.dry_run && dtype != pool.shape->dtype)) return APAR_ERR_INVALID_ARG;
     if (n_cand < 0 || n_cand > 8 || (n_cand > 0 && (m || where != APAR_ROWS_NEXT))) return APAR_ERR_INVALID_ARG;
     if (n == 0) return APAR_OK;
     if (!threads || (n_cand == 0 && mask_dev)) return APAR_ERR_INVALID_ARG;

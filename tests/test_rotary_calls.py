@@ -80,3 +80,15 @@ def test_tensors_of_several_devices_are_refused():
                     lambda: ap.apar_rotate_rows(rot.handle, positions(3), OnGpu(x), OnGpu(y, "cuda:1"), stream=0)):
             with pytest.raises(ValueError):
                 bad()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "bf16_fp8kv", "bf16_fp4kv"])
+def test_bookkeeping_pools_of_every_type_check_listed_threads(dtype):
+    """(There are no rows, and so no type of rows to compare with the pool's.)"""
+    with ap.Pool(4, 2, 128, dtype, 8, dry_run=True) as pool, ap.Rotary(128) as rot:
+        th = ap.apar_thread_create(pool.handle)
+        ap.apar_append_kv(pool.handle, th, None, None, 5)
+        ap.apar_rotate_threads(pool.handle, rot.handle, [th, th], None)
+        ap.apar_rotate_threads(pool.handle, rot.handle, [th], None, m=[5], where=ap.APAR_ROWS_LAST)
+        assert status(lambda: ap.apar_rotate_threads(pool.handle, rot.handle, [th], None, m=[6], where=ap.APAR_ROWS_LAST)) == -1
+        assert status(lambda: ap.apar_rotate_threads(pool.handle, rot.handle, [9], None)) == -2
