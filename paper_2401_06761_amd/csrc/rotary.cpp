@@ -27,9 +27,9 @@ int rotary_rows(const apar_rotary& r, const apar_rotary_rows* x, RotaryRows& out
     return APAR_OK;
 }
 
-// Launches on the device that `on` lies on.
-int rotary_launch(const apar_rotary& r, const RotaryArgs& args, RotaryCall& call, bool f32, int transposed, const void* on, void* hip_stream) {
-    if ((int64_t)(call.q.n_heads + call.k.n_heads) * r.cfg.head_dim > INT32_MAX / 4) return APAR_ERR_UNSUPPORTED;
+// The last checks of a call, and what it takes from the handle.  Nothing is enqueued before them.
+int rotary_ready(const apar_rotary& r, RotaryCall& call, bool f32, int transposed) {
+    if (((int64_t)call.q.n_heads + call.k.n_heads) * r.cfg.head_dim > INT32_MAX / 4) return APAR_ERR_UNSUPPORTED;
     const uintptr_t odd = (uintptr_t)call.q.in | (uintptr_t)call.q.out | (uintptr_t)call.k.in | (uintptr_t)call.k.out;
     if (odd & (f32 ? 3 : 1)) return APAR_ERR_INVALID_ARG;
     call.head_dim = r.cfg.head_dim;
@@ -37,6 +37,11 @@ int rotary_launch(const apar_rotary& r, const RotaryArgs& args, RotaryCall& call
     call.pairs = r.cfg.layout == APAR_ROTARY_PAIRS;
     call.transposed = transposed != 0;
     call.magnitude = (float)r.cfg.magnitude;
+    return APAR_OK;
+}
+
+// Launches on the device that `on` lies on.
+int rotary_launch(const RotaryArgs& args, const RotaryCall& call, bool f32, const void* on, void* hip_stream) {
     DeviceOf guard(on);
     HIP_TRY(launch_rotate_rows(args, call, f32, (hipStream_t)hip_stream));
     return APAR_OK;
@@ -101,17 +106,19 @@ int rotate_threads(apar_pool* p, const apar_rotary* r, int dtype, const apar_thr
     if (pool.dry_run || call.n_rows == 0) return APAR_OK;
     call.mask = mask_dev;
     const bool f32 = dtype == APAR_F32;
+    if ((rc = rotary_ready(*r, call, f32, transposed)) != APAR_OK) return rc;
     if (words.size() <= (size_t)kRotaryInlineWords) {
         RotaryArgs args = r->args;
         memcpy(args.words, words.data(), words.size() * sizeof(int32_t));
-        return rotary_launch(*r, args, call, f32, transposed, pool.kv, hip_stream);
+        return rotary_launch(args, call, f32, pool.kv, hip_stream);
     }
     DeviceGuard guard(pool.device);
     StagedWords staged{};
     if ((rc = stage_words(p, words.data(), words.size(), (hipStream_t)hip_stream, &staged)) != APAR_OK) return rc;
     call.tables = staged.dev;
-    if ((rc = rotary_launch(*r, r->args, call, f32, transposed, pool.kv, hip_stream)) != APAR_OK) return rc;
-    return staged_words_read(staged, (hipStream_t)hip_stream);
+    rc = rotary_launch(r->args, call, f32, pool.kv, hip_stream);
+    const int read = staged_words_read(staged, (hipStream_t)hip_stream);  // (without a kernel too: the upload is under way)
+    return rc != APAR_OK ? rc : read;
 }
 
 }  // namespace
@@ -179,7 +186,8 @@ int apar_rotate_rows(const apar_rotary* r, int dtype, const int32_t* positions_d
     if ((rc = rotary_rows(*r, q, call.q)) != APAR_OK || (rc = rotary_rows(*r, k, call.k)) != APAR_OK) return rc;
     call.positions = positions_dev;
     call.n_rows = n_rows;
-    return rotary_launch(*r, r->args, call, dtype == APAR_F32, transposed, positions_dev, hip_stream);
+    if ((rc = rotary_ready(*r, call, dtype == APAR_F32, transposed)) != APAR_OK) return rc;
+    return rotary_launch(r->args, call, dtype == APAR_F32, positions_dev, hip_stream);
 }
 
 int apar_rotate_threads(apar_pool* p, const apar_rotary* r, int dtype, const apar_thread* threads, const int32_t* m, int n, int where,

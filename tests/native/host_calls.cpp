@@ -1,12 +1,52 @@
-// What calls hand on to the kernels, against the runtime of host_pool.cpp.  Built and run by tests/test_host_calls.py, which names the
-// check to run.
+// What calls hand on to the kernels, and what a call that fails leaves behind, against the runtime of host_pool.cpp.  Built and run by
+// tests/test_host_calls.py, which names the check to run.
 #include "apar_internal.hpp"
+#include "rotary.hpp"
 
 #define main host_pool_main
 #define launch_append_blocks append_nothing
+#define hipMemcpyAsync copy_at_once
+#define hipEventRecord record_nothing
+#define hipEventSynchronize wait_for_nothing
 #include "host_pool.cpp"
 #undef main
 #undef launch_append_blocks
+#undef hipMemcpyAsync
+#undef hipEventRecord
+#undef hipEventSynchronize
+
+// Copies to the device that may still be under way: until an event recorded behind one has been waited for, what it reads must not change.
+struct Upload {
+    const void* from;
+    std::vector<char> was;
+    long at;
+};
+static std::vector<Upload> g_uploads;
+static std::map<hipEvent_t, long> g_recorded;
+static long g_enqueued = 0;
+extern "C" {
+hipError_t hipMemcpyAsync(void* d, const void* s, size_t n, hipMemcpyKind, hipStream_t) {
+    std::memcpy(d, s, n);
+    g_uploads.push_back(Upload{s, std::vector<char>((const char*)s, (const char*)s + n), ++g_enqueued});
+    return hipSuccess;
+}
+hipError_t hipEventRecord(hipEvent_t e, hipStream_t) {
+    g_recorded[e] = g_enqueued;
+    return hipSuccess;
+}
+hipError_t hipEventSynchronize(hipEvent_t e) {
+    const long done = g_recorded[e];
+    g_uploads.erase(std::remove_if(g_uploads.begin(), g_uploads.end(), [&](const Upload& u) { return u.at <= done; }), g_uploads.end());
+    return hipSuccess;
+}
+hipError_t hipGetDeviceCount(int* n) {
+    *n = 1;
+    return hipSuccess;
+}
+}
+static void uploads_unchanged() {
+    for (const Upload& u : g_uploads) CHECK(std::memcmp(u.from, u.was.data(), u.was.size()) == 0);
+}
 
 static std::vector<const char*> g_k, g_v;  // the rows of every append so far
 namespace apar {
@@ -14,6 +54,12 @@ hipError_t launch_append_blocks(const Shape&, void*, const void* k, const void* 
     g_k.push_back((const char*)k);
     g_v.push_back((const char*)v);
     return hipGetLastError();
+}
+static hipError_t g_rotation = hipSuccess;  // what the next launches give
+static int g_rotations = 0;
+hipError_t launch_rotate_rows(const RotaryArgs&, RotaryCall, bool, hipStream_t) {
+    g_rotations += g_rotation == hipSuccess;
+    return g_rotation;
 }
 }  // namespace apar
 
@@ -47,8 +93,44 @@ static void admission() {
         }
 }
 
+// Calls whose tables are uploaded and that are refused or cannot launch: nothing that the upload reads is written while it may be under way.
+static void failures() {
+    apar_pool* p;
+    CHECK(create(4, 2, APAR_BF16, 2000, &p) == APAR_OK);
+    std::vector<apar_thread> ids;
+    for (int i = 0; i < 1500; ++i) ids.push_back(thread_of(p, 1 + i % 16));
+    apar_rotary_config cfg{};
+    cfg.head_dim = cfg.rotary_dim = 128;
+    cfg.base = 10000.0, cfg.magnitude = 1.0;
+    apar_rotary* r;
+    CHECK(apar_rotary_create(&cfg, &r) == APAR_OK);
+    apar_rotary_rows q{}, k{}, odd{}, many{};
+    q.in_dev = q.out_dev = kRows, q.in_stride = q.out_stride = 4 * 128, q.n_heads = 4;
+    k.in_dev = k.out_dev = kRows, k.in_stride = k.out_stride = 2 * 128, k.n_heads = 2;
+    odd = q;
+    odd.in_dev = odd.out_dev = g_kv + 1;
+    auto rotate = [&](int first, const apar_rotary_rows& x) {
+        return apar_rotate_threads(p, r, APAR_BF16, ids.data() + first, nullptr, 1000, APAR_ROWS_NEXT, nullptr, 0, &x, &k, 0, nullptr);
+    };
+    g_uploads.clear();
+    for (int i = 0; i < 3; ++i) {
+        const size_t under_way = g_uploads.size();
+        CHECK(rotate(i, odd) == APAR_ERR_INVALID_ARG);
+        CHECK(g_uploads.size() == under_way);  // (refused before anything is enqueued)
+        apar::g_rotation = hipErrorInvalidValue;
+        CHECK(rotate(i + 1, q) == APAR_ERR_HIP);
+        apar::g_rotation = hipSuccess;
+        for (int next = 0; next < 20; ++next) {
+            CHECK(rotate(next * 20, q) == APAR_OK);
+            uploads_unchanged();
+        }
+    }
+    CHECK(apar::g_rotations == 60);
+    CHECK(apar_rotary_destroy(r) == APAR_OK && apar_pool_destroy(p) == APAR_OK);
+}
+
 int main(int argc, char** argv) {
-    const std::map<std::string, void (*)()> checks = {{"admission", admission}};
+    const std::map<std::string, void (*)()> checks = {{"admission", admission}, {"failures", failures}};
     CHECK(argc == 2 && checks.count(argv[1]));
     checks.at(argv[1])();
     std::printf("ok: %s\n", argv[1]);

@@ -1,4 +1,4 @@
-"""What calls hand on to the kernels: the host side against a HIP runtime that runs on the host (tests/native/host_calls.cpp)."""
+"""What calls hand on to the kernels, and what one that fails leaves behind: the host side against a HIP runtime that runs on the host (tests/native/host_calls.cpp)."""
 import os
 import shutil
 import subprocess
@@ -17,12 +17,12 @@ def host_calls(tmp_path_factory):
     exe = str(tmp_path_factory.mktemp("native") / "host_calls")
     built = subprocess.run([cxx, "-std=c++17", "-O1", "-g", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-I" + os.path.join(ROOT, "include"),
                             "-I" + csrc, os.path.join(ROOT, "tests", "native", "host_calls.cpp")] +
-                           [os.path.join(csrc, f) for f in ("plan.cpp", "apar_pool.cpp", "controller.cpp")] + ["-o", exe], capture_output=True, text=True)
+                           [os.path.join(csrc, f) for f in ("plan.cpp", "apar_pool.cpp", "controller.cpp", "rotary.cpp")] + ["-o", exe], capture_output=True, text=True)
     assert built.returncode == 0, built.stderr[-3000:]
     return exe
 
 
-@pytest.mark.parametrize("check", ["admission"])
+@pytest.mark.parametrize("check", ["admission", "failures"])
 def test_host_side(host_calls, check):
     ran = subprocess.run([host_calls, check], capture_output=True, text=True, timeout=120)
     assert ran.returncode == 0 and ran.stdout == f"ok: {check}\n", ran.stdout + ran.stderr
