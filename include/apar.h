@@ -328,7 +328,7 @@ APAR_API int apar_rotary_destroy(apar_rotary* rotary); /* NULL is accepted */
 /* theta_i as the calls use it; n_out is always set (INVALID_ARG if cap is too small). */
 APAR_API int apar_rotary_frequencies(const apar_rotary* rotary, double* out, int cap, int* n_out);
 /* Rows at positions_dev[0 .. n_rows) (device; any int32).  dtype: APAR_F32 or APAR_BF16, of both; q or k may be NULL.  One launch, nothing
- * allocated: may be captured into a graph.  Errors: INVALID_ARG, UNSUPPORTED, HIP. */
+ * allocated: may be captured into a graph.  Errors: INVALID_ARG, UNSUPPORTED (more than 2^26 - 4 rows), HIP. */
 APAR_API int apar_rotate_rows(const apar_rotary* rotary, int dtype, const int32_t* positions_dev, int64_t n_rows,
                               const apar_rotary_rows* q, const apar_rotary_rows* k, int transposed, void* hip_stream);
 /*
@@ -341,7 +341,7 @@ APAR_API int apar_rotate_rows(const apar_rotary* rotary, int dtype, const int32_
  * dtype (of the rows: APAR_F32 on fp32 pools, APAR_BF16 on the others), numbers of heads and head_dim are the pool's.  Enqueues one launch,
  * and an upload of a word or two per thread where there are more than some 250 of them.  On a dry-run pool q, k and mask_dev are NULL
  * and dtype says nothing.
- * Errors: INVALID_THREAD, INVALID_ARG, UNSUPPORTED (positions or rows past 2^31), HIP.
+ * Errors: INVALID_THREAD, INVALID_ARG, UNSUPPORTED (positions past 2^31, more rows than apar_rotate_rows takes), HIP.
  */
 enum { APAR_ROWS_NEXT = 0, APAR_ROWS_LAST = 1 };
 APAR_API int apar_rotate_threads(apar_pool* pool, const apar_rotary* rotary, int dtype, const apar_thread* threads, const int32_t* m, int n, int where,
@@ -444,7 +444,7 @@ typedef struct apar_sample_row { /* one row's parameters, on the device */
 typedef struct apar_token_ids { /* the vocabulary's numbers of the control tokens (-1: none), which come out as APAR_TOKEN_* ... */
     int32_t fork, child, eos;   /* ... (apar_group_step takes no sampled [Child]: its logit should be -inf)                    */
 } apar_token_ids;
-/* Device memory that a call of n rows wants.  Errors: INVALID_ARG, UNSUPPORTED (vocab > 2^20). */
+/* Device memory that a call of n rows wants.  Errors: INVALID_ARG, UNSUPPORTED (vocab > 2^20, n >= 2^22). */
 APAR_API int apar_sample_workspace_bytes(int n, int vocab, size_t* bytes_out);
 /*
  *   logits_dev   : [n, vocab] of dtype (APAR_F32 or APAR_BF16), rows row_stride elements apart
@@ -455,7 +455,7 @@ APAR_API int apar_sample_workspace_bytes(int n, int vocab, size_t* bytes_out);
  *   workspace_dev: 16-byte aligned; nothing in it has to be set, and nothing is kept in it.  Calls that may overlap (other streams,
  *                  replayed graphs) need one each.
  * Enqueues kernels only: may be captured into a graph.
- * Errors: INVALID_ARG, UNSUPPORTED (vocab > 2^20), WORKSPACE_LIMIT (too small a workspace), HIP.
+ * Errors: INVALID_ARG, UNSUPPORTED (vocab > 2^20, n >= 2^22), WORKSPACE_LIMIT (too small a workspace), HIP.
  */
 APAR_API int apar_sample_tokens(const void* logits_dev, int dtype, int n, int vocab, int64_t row_stride,
                                 const apar_sample_row* rows_dev, const float* uniforms_dev, const apar_token_ids* ids,

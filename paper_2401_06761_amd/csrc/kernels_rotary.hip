@@ -145,9 +145,9 @@ hipError_t launch_rotate_rows(const RotaryArgs& args, RotaryCall call, bool f32,
     };
     const bool vec = call.rotary_dim % (2 * w) == 0 && call.head_dim % (2 * w) == 0 && wide(call.q) && wide(call.k);
     // Rows per workgroup: enough workgroups for the chip first, then rows that keep all threads at sines and cosines.
-    call.rows_per_wg = call.n_rows >= 2048 ? 4 : call.n_rows >= 1024 ? 2 : 1;
+    call.rows_per_wg = call.n_rows >= 2048 ? kRotaryMostRowsPerWg : call.n_rows >= 1024 ? 2 : 1;
     const int64_t grid = (call.n_rows + call.rows_per_wg - 1) / call.rows_per_wg;
-    if (grid > 0x7fffffff) return hipErrorInvalidValue;
+    if (call.n_rows > kRotaryMaxRows) return hipErrorInvalidValue;
     const size_t lds = (size_t)call.rows_per_wg * (call.rotary_dim / 2) * sizeof(f32x2);
 #define APAR_ROTATE(TV, WV, PV) hipLaunchKernelGGL((rotate_rows<TV, WV, PV>), dim3((unsigned)grid), dim3(256), lds, st, args, call)
 #define APAR_ROTATE_PAIRS(TV, WV)                 \

@@ -29,6 +29,7 @@ int rotary_rows(const apar_rotary& r, const apar_rotary_rows* x, RotaryRows& out
 
 // The last checks of a call, and what it takes from the handle.  Nothing is enqueued before them.
 int rotary_ready(const apar_rotary& r, RotaryCall& call, bool f32, int transposed) {
+    if (call.n_rows > kRotaryMaxRows) return APAR_ERR_UNSUPPORTED;
     if (((int64_t)call.q.n_heads + call.k.n_heads) * r.cfg.head_dim > INT32_MAX / 4) return APAR_ERR_UNSUPPORTED;
     const uintptr_t odd = (uintptr_t)call.q.in | (uintptr_t)call.q.out | (uintptr_t)call.k.in | (uintptr_t)call.k.out;
     if (odd & (f32 ? 3 : 1)) return APAR_ERR_INVALID_ARG;

@@ -10,6 +10,8 @@ namespace apar {
 
 constexpr int kRotaryMaxPairs = 128;
 constexpr int kRotaryInlineWords = 512;
+constexpr int kRotaryMostRowsPerWg = 4;
+constexpr int64_t kRotaryMaxRows = (int64_t)kRotaryMostRowsPerWg * ((1 << 24) - 1);  // (a launch has fewer than 2^32 threads)
 
 struct RotaryArgs {                       // the kernel's first argument, read from the head of the argument segment
     double theta[kRotaryMaxPairs];        // turns per position

@@ -9,7 +9,7 @@ extern "C" {
 
 int apar_sample_workspace_bytes(int n, int vocab, size_t* bytes_out) {
     if (!bytes_out || n < 0 || vocab < 1) return APAR_ERR_INVALID_ARG;
-    if (vocab > kSampleMaxVocab) return APAR_ERR_UNSUPPORTED;
+    if (vocab > kSampleMaxVocab || n > kSampleMaxRows) return APAR_ERR_UNSUPPORTED;
     *bytes_out = 0;
     return APAR_OK;
 }
@@ -18,7 +18,7 @@ int apar_sample_tokens(const void* logits_dev, int dtype, int n, int vocab, int6
                        const float* uniforms_dev, const apar_token_ids* ids, int32_t* tokens_dev, float* logprobs_dev,
                        void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
     if (n < 0 || vocab < 1 || (dtype != APAR_F32 && dtype != APAR_BF16)) return APAR_ERR_INVALID_ARG;
-    if (vocab > kSampleMaxVocab) return APAR_ERR_UNSUPPORTED;
+    if (vocab > kSampleMaxVocab || n > kSampleMaxRows) return APAR_ERR_UNSUPPORTED;
     if (n == 0) return APAR_OK;
     if (!logits_dev || !uniforms_dev || !tokens_dev || row_stride < vocab) return APAR_ERR_INVALID_ARG;
     size_t need = 0;

@@ -9,6 +9,7 @@
 namespace apar {
 
 constexpr int kSampleMaxVocab = 1 << 20;
+constexpr int kSampleMaxRows = (1 << 22) - 1;  // (a workgroup of 1024 threads each, and a launch has fewer than 2^32)
 
 struct SampleCall {
     const void* logits;
