@@ -110,7 +110,10 @@ class ServingRun:
         u = torch.from_numpy(uniforms(seeds, batch["seq_index"], batch["length"]).astype(np.float32)).to(logits.device)
         tokens = torch.empty(n, dtype=torch.int32, device=logits.device)
         ap.apar_sample_tokens(logits, u, tokens, self.rows[:n], token_ids=self.token_ids)
-        return np.where(batch["length"] + 1 >= cfg.max_len, EOS, tokens.cpu().numpy()).astype(np.int32)
+        drawn = np.where(batch["length"] + 1 >= cfg.max_len, EOS, tokens.cpu().numpy()).astype(np.int32)
+        if (drawn == ap.APAR_TOKEN_NONE).any():
+            raise RuntimeError(f"no token to draw for threads {batch['thread'][drawn == ap.APAR_TOKEN_NONE].tolist()}: their logits are -inf and NaN")
+        return drawn
 
     def run(self, max_steps: int = 1 << 30) -> dict:
         t0 = time.perf_counter()

@@ -123,3 +123,31 @@ def test_serving_loop_attention_and_books(dtype, n_blocks, max_running, drawn):
     assert (o.preemptions > 0) == (n_blocks < 100) and sum(t["n_forked"] for t in run.trace) > 0
     run.close()
     pool.close()
+
+
+def test_a_row_of_logits_without_a_token_ends_the_loop_with_an_error():
+    """(APAR_TOKEN_NONE is no token that a sequence may go on from.)"""
+    import torch
+
+    reqs = make_requests(3, seed=5, prompt_lo=8, prompt_hi=20)
+    banks = [torch.randn((n, h, 128), device="cuda:0").bfloat16() for n, h in ((64, 4), (256, 2), (256, 2))]
+    bad = []
+
+    def logits(batch, out):
+        x = torch.zeros((len(batch), 50), device="cuda:0")
+        x[bad] = float("nan")
+        return x
+
+    with ap.Pool(4, 2, 128, "bf16_fp4kv", 64, max_threads=1 << 20) as pool:
+        run = ServingRun(pool, reqs, CFG, 4, 1, banks=banks, logits=logits, token_ids=(47, 48, 49))
+        run.keep_trace = True
+        assert run.step()
+        lens = [ap.apar_thread_len(pool.handle, t) for t in run.trace[-1]["threads"]]
+        bad.append(1)
+        with pytest.raises(RuntimeError, match="no token"):
+            run.step()
+        assert lens == [ap.apar_thread_len(pool.handle, t) for t in run.trace[-1]["threads"]] and len(run.trace) == 1  # (nothing was applied)
+        bad.clear()
+        assert run.step()
+        assert all(0 <= x < 50 or -3 <= x < 0 for t in run.trace for x in t["sampled"])
+        run.close()
