@@ -1490,7 +1490,7 @@ int apar_read_kv_rows(apar_pool* p, apar_thread thread, int64_t first, int n, vo
     if (!p || n < 0 || first < 0) return APAR_ERR_INVALID_ARG;
     Thread* t = live_thread(p, thread);
     if (!t) return APAR_ERR_INVALID_THREAD;
-    if (first + n > t->len || p->dry_run) return APAR_ERR_INVALID_ARG;
+    if (first > t->len - n || p->dry_run) return APAR_ERR_INVALID_ARG;
     if (n == 0) return APAR_OK;
     if (!k_out_dev || !v_out_dev) return APAR_ERR_INVALID_ARG;
     DeviceGuard guard(p->device);

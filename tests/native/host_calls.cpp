@@ -5,12 +5,14 @@
 
 #define main host_pool_main
 #define launch_append_blocks append_nothing
+#define launch_read_rows read_nothing
 #define hipMemcpyAsync copy_at_once
 #define hipEventRecord record_nothing
 #define hipEventSynchronize wait_for_nothing
 #include "host_pool.cpp"
 #undef main
 #undef launch_append_blocks
+#undef launch_read_rows
 #undef hipMemcpyAsync
 #undef hipEventRecord
 #undef hipEventSynchronize
@@ -55,6 +57,7 @@ hipError_t launch_append_blocks(const Shape&, void*, const void* k, const void* 
     g_v.push_back((const char*)v);
     return hipGetLastError();
 }
+hipError_t launch_read_rows(const Shape&, const void*, const int32_t*, int, void*, void*, hipStream_t) { return hipGetLastError(); }
 static hipError_t g_rotation = hipSuccess;  // what the next launches give
 static int g_rotations = 0;
 hipError_t launch_rotate_rows(const RotaryArgs&, RotaryCall, bool, hipStream_t) {
@@ -129,8 +132,23 @@ static void failures() {
     CHECK(apar_rotary_destroy(r) == APAR_OK && apar_pool_destroy(p) == APAR_OK);
 }
 
+// Reads past a thread's rows are refused, however far past.
+static void reads() {
+    for (int dtype : {APAR_F32, APAR_BF16, APAR_BF16_FP8KV, APAR_BF16_FP4KV}) {
+        apar_pool* p;
+        CHECK(create(4, 2, dtype, 2000, &p) == APAR_OK);
+        const apar_thread t = thread_of(p, 100);
+        struct { int64_t first; int n, status; } const calls[] = {
+            {0, 100, APAR_OK}, {99, 1, APAR_OK}, {100, 0, APAR_OK}, {0, 101, APAR_ERR_INVALID_ARG}, {100, 1, APAR_ERR_INVALID_ARG},
+            {INT64_MAX, 1, APAR_ERR_INVALID_ARG}, {INT64_MAX - 5, 100, APAR_ERR_INVALID_ARG}, {INT64_MAX, INT32_MAX, APAR_ERR_INVALID_ARG},
+            {INT64_MAX, 0, APAR_ERR_INVALID_ARG}, {-1, 1, APAR_ERR_INVALID_ARG}, {0, -1, APAR_ERR_INVALID_ARG}};
+        for (const auto& c : calls) CHECK(apar_read_kv_rows(p, t, c.first, c.n, kRows, kRows, nullptr) == c.status);
+        CHECK(apar_pool_destroy(p) == APAR_OK);
+    }
+}
+
 int main(int argc, char** argv) {
-    const std::map<std::string, void (*)()> checks = {{"admission", admission}, {"failures", failures}};
+    const std::map<std::string, void (*)()> checks = {{"admission", admission}, {"failures", failures}, {"reads", reads}};
     CHECK(argc == 2 && checks.count(argv[1]));
     checks.at(argv[1])();
     std::printf("ok: %s\n", argv[1]);
