@@ -64,6 +64,9 @@ class ServingRun:
             if st.n_waiting == 0:
                 return False
             raise RuntimeError("the head of the queue does not fit an empty pool")
+        if self.banks is not None and ((2 * n > rows_cap and n + int((batch["last_token"] == FORK).sum()) > rows_cap)
+                                       or (self.attention and n > q.shape[0])):
+            raise ValueError(f"the banks hold {q.shape[0]} queries and {rows_cap} rows, a step of {n} sequences needs more")
         if self.attention:
             if self.out is None or self.out.shape[0] < n:
                 self.out = q.new_empty((max(n, q.shape[0]),) + tuple(q.shape[1:]))

@@ -151,3 +151,19 @@ def test_a_row_of_logits_without_a_token_ends_the_loop_with_an_error():
         assert run.step()
         assert all(0 <= x < 50 or -3 <= x < 0 for t in run.trace for x in t["sampled"])
         run.close()
+
+
+@pytest.mark.parametrize("queries,rows", [(3, 256), (64, 20)])
+def test_banks_that_are_too_small_for_a_step_are_refused(queries, rows):
+    """(Four requests that fork: the step that needs a fourth query, or a 21st row, is not run.)"""
+    import torch
+
+    reqs = make_requests(4, seed=5, prompt_lo=4, prompt_hi=5)
+    cfg = SamplerConfig(p_fork=0.5, p_eos=0.0, max_threads=8, min_new=10, max_len=140)
+    banks = [torch.randn((n, h, 128), device="cuda:0").bfloat16() for n, h in ((queries, 4), (rows, 2), (rows, 2))]
+    with ap.Pool(4, 2, 128, "bf16_fp4kv", 400, max_threads=1 << 20) as pool:
+        run = ServingRun(pool, reqs, cfg, 4, 1, banks=banks)
+        with pytest.raises(ValueError, match="banks"):
+            for _ in range(200):
+                assert run.step()
+        run.close()
