@@ -380,15 +380,17 @@ def _row_step(t) -> Tuple[int, int]:
     heads, d = shape[-2], shape[-1]
     if (d > 1 and stride[-1] != 1) or (heads > 1 and stride[-2] != d):
         raise ValueError("the heads of a row must lie side by side")
-    n, step = 1, heads * d
-    for size, apart in zip(shape[-3::-1], stride[-3::-1]):  # leading dims, the last one first; one of size 1 has no say
-        if size == 1:
-            continue
-        if n == 1:
-            step = apart
-        elif n > 0 and size > 0 and apart != n * step:
-            raise ValueError("rows must be evenly spaced")
-        n *= size
+    n, step = shape[-3], stride[-3]
+    if len(shape) > 3:
+        n = 1
+        for size, apart in zip(shape[-3::-1], stride[-3::-1]):  # leading dims, the last one first; one of size 1 has no say
+            if size == 1:
+                continue
+            if n == 1:
+                step = apart
+            elif n > 0 and size > 0 and apart != n * step:
+                raise ValueError("rows must be evenly spaced")
+            n *= size
     if n > 1 and step < heads * d:
         raise ValueError("rows must not overlap")
     return n, (step if n > 1 else heads * d)
@@ -403,12 +405,12 @@ def _rotary_rows(x, out, n_rows: int):
     n, step = _row_step(x)
     if n != n_rows:
         raise ValueError(f"{n} rows where {n_rows} are meant")
-    at = x.data_ptr()
+    at, shape = x.data_ptr(), x.shape
     if out is None or out is x:
-        return AparRotaryRows(at, at, step, step, *x.shape[-2:])
-    if out.shape != x.shape or out.dtype != x.dtype or out.device != x.device:
+        return AparRotaryRows(at, at, step, step, shape[-2], shape[-1])
+    if out.shape != shape or out.dtype != x.dtype or out.get_device() != x.get_device():
         raise ValueError("the output must have its input's shape, type and device")
-    return AparRotaryRows(at, out.data_ptr(), step, _row_step(out)[1], *x.shape[-2:])
+    return AparRotaryRows(at, out.data_ptr(), step, _row_step(out)[1], shape[-2], shape[-1])
 
 
 def _stream_on(t, stream) -> int:
@@ -445,9 +447,9 @@ def apar_rotate_rows(rotary, positions, q, k=None, q_out=None, k_out=None, trans
         raise ValueError("positions must be a 1-d int32 tensor")
     if q is None and k is None:
         raise ValueError("neither q nor k")
-    n, device = positions.shape[0], positions.device
+    n, device = positions.shape[0], positions.get_device()
     qr, kr = _rotary_rows(q, q_out, n), _rotary_rows(k, k_out, n)
-    if (q is not None and q.device != device) or (k is not None and k.device != device):
+    if (q is not None and q.get_device() != device) or (k is not None and k.get_device() != device):
         raise ValueError("all tensors must be on one device")
     _check(_L().apar_rotate_rows(rotary, _rows_dtype(q, k), _ptr(positions), n, qr, kr, int(bool(transposed)),
                                  _stream_on(positions, stream)), "apar_rotate_rows")
@@ -468,8 +470,10 @@ def apar_rotate_threads(pool, rotary, threads: Sequence[int], q, k=None, q_out=N
     if mask is not None and (mask.element_size() != 1 or mask.numel() != rows):
         raise ValueError("mask must hold one byte per candidate")
     one = q if q is not None else k
-    if one is not None and ((k is not None and k.device != one.device) or (mask is not None and mask.device != one.device)):
-        raise ValueError("all tensors must be on one device")
+    if one is not None:
+        device = one.get_device()
+        if (k is not None and k.get_device() != device) or (mask is not None and mask.get_device() != device):
+            raise ValueError("all tensors must be on one device")
     _check(_L().apar_rotate_threads(pool, rotary, dtype, arr, marr, n, where, _ptr(mask), n_cand, qr, kr, int(bool(transposed)),
                                     _stream_on(one, stream)), "apar_rotate_threads")
 

@@ -15,6 +15,9 @@ class OnGpu:
         self.t, self.device = t, torch.device(device)
         self.shape, self.dtype = t.shape, t.dtype
 
+    def get_device(self):
+        return self.device.index
+
     def __getattr__(self, name):
         return getattr(self.t, name)
 
