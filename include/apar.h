@@ -239,6 +239,8 @@ APAR_API int apar_decode_attention_spec(apar_pool* pool, const void* q_dev, cons
  * in it has to start at zero (a call overwrites every table and every partial result it reads),
  * but two fixed calls that overlap on one GPU - different streams, or different pools, without an
  * order between them - race on it.  Calls on one stream are ordered by the stream.
+ * Under capture: a pool's first fixed call can be captured (waiting for the upload of an earlier one is not allowed there: HIP),
+ * its replays read the plan from the pool's staging buffer, and a pool with a captured call should make no other fixed call.
  * Errors: as apar_decode_attention, plus WORKSPACE_LIMIT, and INVALID_ARG on a dry-run pool.
  */
 #define APAR_FIXED_PLAN_BYTES (2 << 20)
@@ -444,7 +446,7 @@ typedef struct apar_sample_row { /* one row's parameters, on the device */
 typedef struct apar_token_ids { /* the vocabulary's numbers of the control tokens (-1: none), which come out as APAR_TOKEN_* ... */
     int32_t fork, child, eos;   /* ... (apar_group_step takes no sampled [Child]: its logit should be -inf)                    */
 } apar_token_ids;
-/* Device memory that a call of n rows wants.  Errors: INVALID_ARG, UNSUPPORTED (vocab > 2^20, n >= 2^22). */
+/* Device memory that a call of n rows wants: 0 for every n and vocab as the kernels are now (workspace_dev may be NULL then).  Errors: INVALID_ARG, UNSUPPORTED (vocab > 2^20, n >= 2^22). */
 APAR_API int apar_sample_workspace_bytes(int n, int vocab, size_t* bytes_out);
 /*
  *   logits_dev   : [n, vocab] of dtype (APAR_F32 or APAR_BF16), rows row_stride elements apart

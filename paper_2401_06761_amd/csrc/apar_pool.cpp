@@ -450,7 +450,7 @@ int send_blocks(apar_pool* p, const std::vector<int32_t>& copies, const void* k,
 constexpr int64_t kFewAgainBytes = (int64_t)56 << 20, kFewAgainWideBytes = (int64_t)112 << 20, kFewAgainNarrowBytes = (int64_t)56 << 20;
 constexpr int64_t kFewSmallBytes = (int64_t)64 << 20;
 constexpr int32_t kFewUnits = 1024;
-// 4-bit pools: 64 requests of six threads, group 8 (1536 units) 47 -> 38 us with units of 16 rows; 24 of eight threads and five candidates (3072)
+// 4-bit pools: 64 requests of six threads, group 8 (1536 units) 47 -> 38 us with units of 16 rows; 24 of eight threads and five candidates (twice as many)
 // 55 -> 60.
 constexpr int32_t kFewUnitsFp4 = 2048;
 // 4-bit pools: the most tiles such units may list (kFewTiles elsewhere), whose reading again costs a quarter: two MiB of table, and one where the

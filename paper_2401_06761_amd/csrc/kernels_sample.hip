@@ -15,13 +15,18 @@
 // runs, then among the 64 values of one.  The row stays in registers for the pass that looks for the token's index.  A value
 // that occurs more than 65535 times shows in the counters' sum; such a row goes through the digits.  Both ways give the same token.
 // What bounds it: memory, behind that the passes over the counters, which nothing fills where a compute unit has one row.
-// (256 rows of 128000 in 24 us, 65 MB; one row of 32000 in 12.5 us, of which 5 are a launch.)
+// (256 rows of 128000 in 23 to 25 us, 65 MB; one row of 32000 in 12 us, with all cuts 15, the largest token alone 8; of these 5 are a launch.)  Rows of more than 131072 tokens
+// are read twice, with nothing on its way (64 rows of 200000 in 33 us).  Tokens of one value meet in one counter, 64 updates of a wavefront
+// one after the other, the masked ones of a row among them: 256 rows of 128000, half of each -inf, 71 us; nine tenths, which go through the
+// digits, 244, of the type's lowest value 382.
 //
 // fp32 rows (sample_rows_f32): every token has a weight of its own.  Its mass goes into one of 8192 bins of equal width between the largest value
 // and the lightest that counts, a few tokens each where the row is dense; the tokens of the bin a target falls into become a list, and a
 // token's place in it comes from comparing all with all.  That is a pass for the range, one for the masses and one per list, where digits
-// take up to three per target and one for the index.  What bounds it: the weights' 64-bit instructions (some fifteen per token; the atomics beside
-// them cost no time of their own).  256 rows of 128000 in 82 us (173 through the digits), one row of 32000 in 23 us (52).
+// take up to three per target and one for the index.  What bounds it: those passes' reads.  256 rows of 128000 with nothing cut are three passes,
+// 393 MB, in 81 us, 4.6 TB/s (173 through the digits), with top-k, top-p and min-p in every row 427 MB in 110; the weights, some fifteen 64-bit
+// instructions per token, keep the vector units busy for half of that time.  A row by itself is one compute unit's: 32000 in 23 to 30 us (52),
+// 128000 in 57 to 73.
 #include <hip/hip_runtime.h>
 
 #include "apar_internal.hpp"
