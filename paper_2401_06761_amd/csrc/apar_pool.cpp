@@ -251,6 +251,15 @@ int acquire_stage(apar_pool* p, size_t bytes, StageSlot** out) {
     return APAR_OK;
 }
 
+// A call that ends early leaves its slot to whatever it has enqueued (an upload, at least).
+struct HeldSlot {
+    StageSlot* s = nullptr;
+    hipStream_t st = nullptr;
+    ~HeldSlot() {
+        if (s && !s->pending) s->pending = hipEventRecord(s->ev, st) == hipSuccess;
+    }
+};
+
 // Uploads the first `bytes` of a staging slot on the pool's own copy stream and makes the caller's stream wait
 // for it: the copy then runs beside whatever the caller's stream is still busy with (the previous step's
 // attention, typically) instead of queueing behind it.  The slot is free by construction: acquire_stage waited
@@ -393,6 +402,7 @@ int send_blocks(apar_pool* p, const std::vector<int32_t>& copies, const void* k,
     }
     const int32_t* tables = (const int32_t*)blocks.data();
     StageSlot* s = nullptr;
+    HeldSlot held{nullptr, st};
     int rc = APAR_OK;
     if (inlined) {
         if (!src.empty()) {
@@ -403,6 +413,7 @@ int send_blocks(apar_pool* p, const std::vector<int32_t>& copies, const void* k,
     } else {
         const size_t total = (words + copy_words) * sizeof(int32_t);
         if ((rc = acquire_stage(p, total, &s)) != APAR_OK) return rc;
+        held.s = s;
         int32_t* host = (int32_t*)s->host;
         memcpy(host, blocks.data(), blocks.size() * sizeof(AppendBlock));
         if (!src.empty()) memcpy(host + blocks.size() * 4, src.data(), src.size() * sizeof(int32_t));
@@ -736,6 +747,7 @@ int decode_common(apar_pool* p, const void* q, const void* cand_k, const void* c
     bool cut = !p->split_blocks.empty();
     const size_t slots = (size_t)ph.n_partial_rows * n_cand * p->shape.n_q;
     StageSlot* s = nullptr;
+    HeldSlot held{nullptr, st};
     char *host = nullptr, *dev = nullptr;
     size_t fixed_bytes = 0;
     PartialBuf part = p->part;
@@ -787,6 +799,7 @@ int decode_common(apar_pool* p, const void* q, const void* cand_k, const void* c
         fixed_bytes = cut ? staged : ofs[5];
     } else if (!inlined) {
         if ((rc = acquire_stage(p, staged, &s)) != APAR_OK) return rc;
+        held.s = s;
         host = s->host;
         dev = s->dev;
     }
@@ -992,6 +1005,7 @@ int prefill_bf16(apar_pool* p, const std::vector<PrefillThreadView>& views, int6
     StageSlot* s = nullptr;
     int rc = acquire_stage(p, wg_bytes + table_bytes, &s);
     if (rc != APAR_OK) return rc;
+    const HeldSlot held{s, st};
     memcpy(s->host, wgs.data(), wgs.size() * sizeof(PrefillWg));
     memcpy(s->host + wg_bytes, tables.data(), table_bytes);
     if ((rc = upload(p, s, wg_bytes + table_bytes, st)) != APAR_OK) return rc;
@@ -1066,6 +1080,7 @@ int prefill_common(apar_pool* p, const void* q, const apar_thread* ids, const in
     const size_t tile_bytes = ph.tiles.size() * sizeof(TileRef);
     StageSlot* s = nullptr;
     if ((rc = acquire_stage(p, wg_bytes + tile_bytes, &s)) != APAR_OK) return rc;
+    const HeldSlot held{s, st};
     memcpy(s->host, ph.wgs.data(), ph.wgs.size() * sizeof(WgDesc));
     if (tile_bytes) memcpy(s->host + wg_bytes, ph.tiles.data(), tile_bytes);
     if ((rc = upload(p, s, wg_bytes + tile_bytes, st)) != APAR_OK) return rc;
@@ -1508,6 +1523,7 @@ int apar_read_kv_rows(apar_pool* p, apar_thread thread, int64_t first, int n, vo
     const size_t words = p->shape.fp4 ? 1 + (size_t)(first % kBlockTokens + n + kBlockTokens - 1) / kBlockTokens : (size_t)n;
     int rc = acquire_stage(p, words * sizeof(int32_t), &s);
     if (rc != APAR_OK) return rc;
+    const HeldSlot held{s, st};
     int32_t* codes = (int32_t*)s->host;
     if (p->shape.fp4) {
         codes[0] = (int32_t)(first % kBlockTokens);

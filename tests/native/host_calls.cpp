@@ -132,6 +132,41 @@ static void failures() {
     CHECK(apar_rotary_destroy(r) == APAR_OK && apar_pool_destroy(p) == APAR_OK);
 }
 
+// The same of the pool's own calls, each with tables that are uploaded.
+static void failed_launches() {
+    for (int dtype : {APAR_F32, APAR_BF16, APAR_BF16_FP4KV})
+        for (int kind = 0; kind < 5; ++kind) {
+            apar_pool* p;
+            CHECK(create(4, 2, dtype, 20000, &p) == APAR_OK);
+            std::vector<apar_thread> ids;
+            for (int i = 0; i < 700; ++i) ids.push_back(thread_of(p, 100 + i % 16));
+            const apar_thread big = thread_of(p, 20000);
+            const std::vector<int32_t> ones(700, 1), pieces(700, 90);
+            auto call = [&](int n) -> int {
+                switch (kind) {
+                    case 0: return apar_append_kv_batch(p, ids.data(), n, kRows, kRows, nullptr);
+                    case 1: return apar_read_kv_rows(p, big, 0, 17000 + n, kRows, kRows, nullptr);
+                    case 2: return apar_decode_attention(p, kRows, ids.data(), n, kRows, nullptr);
+                    case 3: return apar_prefill_attention(p, kRows, ids.data(), ones.data(), n, kRows, nullptr);
+                    default: return apar_prefill_attention(p, kRows, ids.data(), pieces.data(), n, kRows, nullptr);
+                }
+            };
+            CHECK(apar_set_plan_reuse(p, 0) == APAR_OK);
+            g_uploads.clear();
+            for (int i = 0; i < 3; ++i) {
+                const long before = g_enqueued;
+                g_last = hipErrorInvalidValue;
+                CHECK(call(690 - i) == APAR_ERR_HIP && g_last == hipSuccess);
+                CHECK(g_enqueued > before);  // (the case is one that uploads)
+                for (int next = 0; next < 12; ++next) {
+                    CHECK(call(500 + next * 10) == APAR_OK);
+                    uploads_unchanged();
+                }
+            }
+            CHECK(apar_pool_destroy(p) == APAR_OK);
+        }
+}
+
 // Reads past a thread's rows are refused, however far past.
 static void reads() {
     for (int dtype : {APAR_F32, APAR_BF16, APAR_BF16_FP8KV, APAR_BF16_FP4KV}) {
@@ -148,7 +183,7 @@ static void reads() {
 }
 
 int main(int argc, char** argv) {
-    const std::map<std::string, void (*)()> checks = {{"admission", admission}, {"failures", failures}, {"reads", reads}};
+    const std::map<std::string, void (*)()> checks = {{"admission", admission}, {"failures", failures}, {"reads", reads}, {"failed_launches", failed_launches}};
     CHECK(argc == 2 && checks.count(argv[1]));
     checks.at(argv[1])();
     std::printf("ok: %s\n", argv[1]);

@@ -22,7 +22,7 @@ def host_calls(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("check", ["admission", "failures", "reads"])
+@pytest.mark.parametrize("check", ["admission", "failures", "reads", "failed_launches"])
 def test_host_side(host_calls, check):
     ran = subprocess.run([host_calls, check], capture_output=True, text=True, timeout=120)
     assert ran.returncode == 0 and ran.stdout == f"ok: {check}\n", ran.stdout + ran.stderr
